@@ -339,6 +339,41 @@ dasgd_status dasgd_destroy(dasgd_ctx *ctx);         /* synchronises both streams
 dasgd_status dasgd_average_merge_noalloc(void *w_device, int32_t K, int64_t P, int64_t ld, float xi,
                                          int32_t device, void *stream, char *errbuf, int64_t errbuf_len);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Operators of language-model replicas.  Like the weights, an embedding table or a weight matrix of a replica
+ * is a contiguous slice of its row: replica k's slice starts at element k*ld + offset of a [K][ld] array.
+ * These calls keep no context between them (the orthogonaliser's plan apart): every call takes the stream it
+ * is enqueued on and returns without waiting; dasgd_last_error(NULL) explains a non-OK status.  T = 0 is valid. */
+typedef enum { DASGD_ELEM_F32 = 0, DASGD_ELEM_BF16 = 1 } dasgd_elem;
+
+typedef struct {
+  int32_t K, V, D;      /* replicas, rows of the table, columns of the table                                   */
+  int32_t device;       /* ordinal of the GPU that holds every buffer                                          */
+  int64_t T;            /* tokens of each replica, 0 <= T < 2^31                                               */
+  int64_t ld, offset;   /* the array that holds the table: row stride and the table's first element (elements);
+                           offset + V*D <= ld                                                                  */
+  float scale;          /* multiplies the rows looked up, and the gradient                                     */
+  int32_t token_bits;   /* 32 or 64: tokens are int32_t or int64_t                                             */
+  int32_t table_elem;   /* dasgd_elem of the array that holds the table (lookup) or its gradient (gradient)    */
+  int32_t rows_elem;    /* dasgd_elem of the [K][T][D] activations (lookup: written, gradient: read)           */
+  int32_t accumulate;   /* gradient: 0 writes every row of the table's gradient (rows no token selects become 0),
+                           1 adds to what is there and leaves the other rows alone                             */
+} dasgd_embed_config;
+
+/* out[k][t][:] = scale * table_k[tokens[k][t]][:] in float32, rounded to the type of out.  tokens: device, [K][T] contiguous; out: device,
+ * [K][T][D] contiguous.  A token outside [0, V) selects nothing: its row of out is zero. */
+dasgd_status dasgd_embed_lookup(const dasgd_embed_config *cfg, const void *table_array_device, const void *tokens_device,
+                                void *out_device, void *stream);
+
+/* dtable_k[v][:] (+)= scale * sum over t with tokens[k][t] = v of dy[k][t][:].  Tokens are sorted on the device,
+ * sums are held in float32 and added in an order that the tokens alone decide (no floating-point atomics: equal
+ * inputs give equal bits), and rounded once.  Tokens outside [0, V) contribute nothing.  workspace: device, 256-byte
+ * aligned, of at least the bytes that dasgd_embed_workspace names (they serve any T up to cfg->T); its contents need not be kept between calls, and calls
+ * that can overlap on the GPU need one each. */
+dasgd_status dasgd_embed_workspace(const dasgd_embed_config *cfg, int64_t *bytes);
+dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy_device, const void *tokens_device,
+                                  void *grad_array_device, void *workspace_device, int64_t workspace_bytes, void *stream);
+
 /* Library version, "major.minor". */
 const char *dasgd_version(void);
 

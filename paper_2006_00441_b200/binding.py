@@ -30,6 +30,7 @@ DASGD_FLAG_FUSE_MERGE_D1 = 0x80
 DASGD_FLAG_TWO_LANES = 0x100
 DASGD_FLAG_GRAPH = 0x200
 DASGD_FLAG_TWO_SIDE_STREAMS = 0x400
+DASGD_ELEM_F32, DASGD_ELEM_BF16 = 0, 1
 
 EXPORTS = [
     "dasgd_init", "dasgd_local_step", "dasgd_snapshot", "dasgd_average_async", "dasgd_merge", "dasgd_sync",
@@ -38,6 +39,7 @@ EXPORTS = [
     "dasgd_average_merge_noalloc", "dasgd_delay_guideline", "dasgd_advise_delay", "dasgd_export_state", "dasgd_import_state",
     "dasgd_get_kernel_units", "dasgd_refresh_lp",
     "dasgd_set_momentum_averaging", "dasgd_get_pending_momentum",
+    "dasgd_embed_lookup", "dasgd_embed_workspace", "dasgd_embed_gradient",
     "dasgd_set_shard", "dasgd_set_shard_nccl", "dasgd_nccl_unique_id", "dasgd_nccl_comm_init", "dasgd_nccl_comm_destroy",
 ]
 
@@ -55,6 +57,15 @@ class dasgd_config(ctypes.Structure):
         ("w", ctypes.c_void_p), ("m", ctypes.c_void_p), ("w_lp", ctypes.c_void_p), ("snap", ctypes.c_void_p),
         ("mean", ctypes.c_void_p), ("g_stage", ctypes.c_void_p),
         ("main_stream", ctypes.c_void_p), ("side_stream", ctypes.c_void_p),
+    ]
+
+
+class dasgd_embed_config(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_int32), ("V", ctypes.c_int32), ("D", ctypes.c_int32), ("device", ctypes.c_int32),
+        ("T", ctypes.c_int64), ("ld", ctypes.c_int64), ("offset", ctypes.c_int64),
+        ("scale", ctypes.c_float), ("token_bits", ctypes.c_int32), ("table_elem", ctypes.c_int32),
+        ("rows_elem", ctypes.c_int32), ("accumulate", ctypes.c_int32),
     ]
 
 
@@ -106,6 +117,10 @@ def _load() -> ctypes.CDLL:
     L.dasgd_nccl_unique_id.argtypes = [vp]
     L.dasgd_nccl_comm_init.argtypes = [ctypes.POINTER(vp), vp, i32, i32, i32]
     L.dasgd_nccl_comm_destroy.argtypes = [vp]
+    pemb = ctypes.POINTER(dasgd_embed_config)
+    L.dasgd_embed_lookup.argtypes = [pemb, vp, vp, vp, vp]
+    L.dasgd_embed_workspace.argtypes = [pemb, ctypes.POINTER(i64)]
+    L.dasgd_embed_gradient.argtypes = [pemb, vp, vp, vp, vp, i64, vp]
     L.dasgd_version.argtypes = []
     L.dasgd_version.restype = ctypes.c_char_p
     return L
@@ -287,6 +302,107 @@ def dasgd_average_merge_noalloc(w_ptr: int, K: int, P: int, ld: int, xi: float, 
     st = _L.dasgd_average_merge_noalloc(w_ptr, K, P, ld, xi, device, stream_ptr, buf, len(buf))
     if st != DASGD_OK:
         raise DasgdError(st, f"{_L.dasgd_strerror(st).decode()}: {buf.value.decode()}")
+
+
+# ---------------------------------------------------------------- operators of language-model replicas
+
+def dasgd_embed_lookup(cfg: dasgd_embed_config, table_array_ptr: int, tokens_ptr: int, out_ptr: int, stream_ptr: int | None):
+    _check(_L.dasgd_embed_lookup(ctypes.byref(cfg), table_array_ptr, tokens_ptr, out_ptr, stream_ptr), None)
+
+
+def dasgd_embed_workspace(cfg: dasgd_embed_config) -> int:
+    n = ctypes.c_int64()
+    _check(_L.dasgd_embed_workspace(ctypes.byref(cfg), ctypes.byref(n)), None)
+    return n.value
+
+
+def dasgd_embed_gradient(cfg: dasgd_embed_config, dy_ptr: int, tokens_ptr: int, grad_array_ptr: int, workspace_ptr: int,
+                         workspace_bytes: int, stream_ptr: int | None):
+    _check(_L.dasgd_embed_gradient(ctypes.byref(cfg), dy_ptr, tokens_ptr, grad_array_ptr, workspace_ptr, workspace_bytes,
+                                   stream_ptr), None)
+
+
+_ELEM = {torch.float32: DASGD_ELEM_F32, torch.bfloat16: DASGD_ELEM_BF16}
+_TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
+
+
+class _StreamOrder:
+    """Calls that share a workspace run one after the other also when the caller changes streams between them."""
+
+    def __init__(self, device):
+        self.device, self.last, self.done = device, torch.cuda.current_stream(device), None
+
+    def enter(self, tensors) -> int:
+        stream = torch.cuda.current_stream(self.device)
+        if self.last != stream:
+            if self.done is None:
+                self.done = torch.cuda.Event()
+            self.done.record(self.last)
+            stream.wait_event(self.done)
+            for t in tensors:
+                t.record_stream(stream)
+        self.last = stream
+        return stream.cuda_stream
+
+
+class Embedding:
+    """The embedding tables of K replicas: ``[V, D]`` slices that start at element ``offset`` of the rows of ``[K, ld]``
+    arrays (``DaSGD.w`` or its bfloat16 copy for the lookup, the gradient array for the gradient).
+
+    Calls are enqueued on torch's current stream of ``device`` and return at once.  Tokens outside ``[0, V)`` (padding)
+    give zero rows and contribute nothing to the gradient.
+    """
+
+    def __init__(self, K, ld, offset, V, D, scale=1.0, max_tokens=0, device=0):
+        if not torch.cuda.is_available():
+            raise RuntimeError("Embedding needs a CUDA device; there is no CPU implementation")
+        self.K, self.ld, self.offset, self.V, self.D, self.max_tokens = K, ld, offset, V, D, max_tokens
+        self.device = torch.device("cuda", device)
+        c = self.cfg = dasgd_embed_config()
+        c.K, c.V, c.D, c.device, c.T, c.ld, c.offset, c.scale = K, V, D, device, max_tokens, ld, offset, scale
+        c.token_bits = 64
+        self._ws = torch.empty(dasgd_embed_workspace(c), dtype=torch.uint8, device=self.device)
+        self._order = _StreamOrder(self.device)
+
+    def _set(self, array, tokens, rows, what):
+        K, D, c = self.K, self.D, self.cfg
+        if not (array.is_cuda and tokens.is_cuda and array.device == tokens.device == self.device):
+            raise ValueError(f"the {what} array and the tokens must be on {self.device}")
+        if array.dtype not in _ELEM or tuple(array.shape) != (K, self.ld) or not array.is_contiguous():
+            raise ValueError(f"the {what} array must be a contiguous float32 or bfloat16 tensor of shape {(K, self.ld)}")
+        if tokens.dtype not in _TOKEN_BITS or tokens.dim() != 2 or tokens.shape[0] != K or not tokens.is_contiguous():
+            raise ValueError(f"tokens must be a contiguous int32 or int64 tensor of shape ({K}, T)")
+        T = tokens.shape[1]
+        if rows is not None and (rows.dtype not in _ELEM or tuple(rows.shape) != (K, T, D) or not rows.is_contiguous()
+                                 or rows.device != self.device):
+            raise ValueError(f"activations must be a contiguous float32 or bfloat16 tensor of shape {(K, T, D)} on {self.device}")
+        c.T, c.token_bits, c.table_elem = T, _TOKEN_BITS[tokens.dtype], _ELEM[array.dtype]
+        return T
+
+    def lookup(self, w, tokens, out=None, out_dtype=None):
+        """``scale * table[tokens]``: ``[K, T, D]`` in ``out`` (made if not given; its type defaults to the table's)."""
+        T = self._set(w, tokens, out, "weight")
+        if out is None:
+            out = torch.empty((self.K, T, self.D), dtype=out_dtype or w.dtype, device=self.device)
+        elif out_dtype is not None and out.dtype != out_dtype:
+            raise ValueError("out and out_dtype disagree")
+        if out.dtype not in _ELEM:
+            raise ValueError("out_dtype must be float32 or bfloat16")
+        self.cfg.rows_elem = _ELEM[out.dtype]
+        dasgd_embed_lookup(self.cfg, w.data_ptr(), tokens.data_ptr(), out.data_ptr(),
+                           torch.cuda.current_stream(self.device).cuda_stream)
+        return out
+
+    def gradient(self, dy, tokens, g, accumulate=False):
+        """Writes the table's slice of ``g`` (all of it, or adds to the rows that tokens select when ``accumulate``)."""
+        T = self._set(g, tokens, dy, "gradient")
+        if T > self.max_tokens:
+            raise ValueError(f"{T} tokens per replica, but max_tokens is {self.max_tokens}")
+        self.cfg.rows_elem, self.cfg.accumulate = _ELEM[dy.dtype], int(accumulate)
+        stream = self._order.enter((self._ws,))
+        dasgd_embed_gradient(self.cfg, dy.data_ptr(), tokens.data_ptr(), g.data_ptr(), self._ws.data_ptr(),
+                             self._ws.numel(), stream)
+        return g
 
 
 # ---------------------------------------------------------------- convenience wrapper

@@ -1,0 +1,213 @@
+"""Embedding lookup and its gradient by sorted tokens against plain 64-bit forms.
+
+Tolerances.  The lookup is one float32 product rounded to the output's type: compared bit for bit.  A gradient element is
+a float32 sum of n terms in some order, so it is within (n - 1) u * sum|x| of the exact sum (u = 2^-24), times the scale,
+one more u for the product, one for the addition to an old value, and half a unit in the last place of the output's type.
+"""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def make(K, T, V, D, gap, tok="zipf", it=torch.int64, seed=0, pad=0.1):
+    gen = torch.Generator("cuda").manual_seed(seed)
+    if tok == "zipf":
+        p = (torch.arange(V, device="cuda", dtype=torch.float64) + 1) ** -1.2
+        t = torch.searchsorted((p / p.sum()).cumsum(0), torch.rand(K, T, generator=gen, device="cuda", dtype=torch.float64)).clamp_(max=V - 1)
+        t = torch.randperm(V, generator=gen, device="cuda")[t]
+    elif tok == "same":
+        t = torch.full((K, T), V - 1, device="cuda")
+    elif tok == "none":
+        t = torch.full((K, T), -1, device="cuda")
+    else:
+        t = torch.randint(0, V, (K, T), generator=gen, device="cuda")
+    if tok != "none" and pad:
+        r = torch.rand(K, T, generator=gen, device="cuda")
+        t = torch.where(r < pad / 2, -1, torch.where(r < pad, V + 3, t))   # both sides of the table
+    return gen, t.to(it), V * D + 2 * gap
+
+
+def valid(t, V):
+    return (t >= 0) & (t < V)
+
+
+@pytest.mark.parametrize("wt", ["f32", "bf16"])
+@pytest.mark.parametrize("ot", ["f32", "bf16"])
+@pytest.mark.parametrize("K,T,V,D,gap,it", [(1, 1, 1, 1, 0, torch.int64), (3, 1, 100, 1024, 0, torch.int32), (2, 77, 513, 333, 5, torch.int64),
+                                            (2, 500, 64, 8, 8, torch.int32), (1, 1000, 1000, 2056, 16, torch.int64), (4, 0, 10, 16, 0, torch.int64)])
+def test_lookup(K, T, V, D, gap, it, wt, ot):
+    from paper_2006_00441_b200 import binding as B
+    gen, tok, ld = make(K, T, V, D, gap, it=it)
+    w = torch.randn(K, ld, generator=gen, device="cuda").to(DT[wt])
+    emb = B.Embedding(K, ld, gap, V, D, scale=1.7)
+    got = emb.lookup(w, tok, out_dtype=DT[ot])
+    table = w[:, gap:gap + V * D].view(K, V, D).float()
+    ok = valid(tok, V)
+    rows = torch.gather(table, 1, tok.long().where(ok, 0)[..., None].expand(K, T, D))
+    want = (rows * torch.tensor(1.7, dtype=torch.float32, device="cuda")).where(ok[..., None], 0.0).to(DT[ot])
+    assert got.dtype == DT[ot] and torch.equal(got, want)
+
+
+def test_lookup_passes_infinities_and_nan_of_selected_rows_only():
+    from paper_2006_00441_b200 import binding as B
+    w = torch.zeros(1, 4 * 8, device="cuda")
+    w.view(4, 8)[1] = float("inf")
+    w.view(4, 8)[2] = float("nan")
+    emb = B.Embedding(1, 32, 0, 4, 8, scale=0.5)
+    out = emb.lookup(w, torch.tensor([[0, 1, 2, -1, 3]], device="cuda"))[0]
+    assert bool((out[[0, 3, 4]] == 0).all()) and bool(out[1].isposinf().all()) and bool(out[2].isnan().all())
+
+
+def half_ulp(x, dtype):
+    """Half a unit in the last place of `dtype` at |x|: bfloat16 keeps 8 significant bits, so 2^(e - 8) for 2^e <= |x| < 2^(e+1)."""
+    return torch.exp2(torch.floor(torch.log2(x.abs().clamp(min=1e-37))) - 8) if dtype == torch.bfloat16 else torch.zeros_like(x)
+
+
+def gradient_reference(dy, tok, V, scale, old):
+    """Exact gradient, and the bound on the float32 sum's error, element by element (64 bits)."""
+    K, T, D = dy.shape
+    want, mag, n = (torch.zeros(K, V, D, dtype=torch.float64, device="cuda") for _ in range(3))
+    for k in range(K):
+        ok = valid(tok[k], V)
+        idx, x = tok[k][ok].long(), dy[k][ok].double()
+        want[k].index_add_(0, idx, x)
+        mag[k].index_add_(0, idx, x.abs())
+        n[k].index_add_(0, idx, torch.ones_like(x))
+    bound = abs(scale) * mag * (n + 1) * U
+    want = want * scale
+    if old is not None:
+        want = want + old.double()
+        bound = bound + 2 * U * (want.abs() + bound)
+    return want, bound
+
+
+CASES = [
+    # K, T, V, D, gap, tokens, int type, pad
+    (1, 1, 1, 1, 0, "zipf", torch.int64, 0.0), (3, 1, 50, 24, 3, "uniform", torch.int32, 0.0), (2, 0, 40, 16, 0, "zipf", torch.int64, 0.0),
+    (2, 31, 7, 8, 8, "zipf", torch.int64, 0.1), (2, 33, 1000, 333, 5, "zipf", torch.int32, 0.1), (1, 1024, 300, 64, 0, "uniform", torch.int64, 0.5),
+    (1, 1025, 300, 72, 0, "same", torch.int64, 0.0), (2, 2049, 70000, 40, 16, "zipf", torch.int64, 0.1), (2, 5000, 259, 264, 0, "zipf", torch.int32, 0.0),
+    (1, 9001, 3, 1024, 0, "uniform", torch.int64, 0.1), (1, 70001, 5003, 16, 0, "zipf", torch.int64, 0.05), (2, 777, 100, 32, 0, "none", torch.int64, 0.0),
+    (5, 640, 511, 520, 8, "zipf", torch.int64, 0.1), (1, 12000, 512, 1032, 0, "same", torch.int32, 0.3), (1, 300, 300000, 8, 0, "uniform", torch.int64, 0.0),
+]
+
+
+@pytest.mark.parametrize("at,gt", [("f32", "f32"), ("bf16", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("acc", [False, True])
+@pytest.mark.parametrize("K,T,V,D,gap,tok,it,pad", CASES)
+def test_gradient(K, T, V, D, gap, tok, it, pad, acc, at, gt):
+    from paper_2006_00441_b200 import binding as B
+    gen, t, ld = make(K, T, V, D, gap, tok, it, seed=T + D, pad=pad)
+    dy = torch.randn(K, T, D, generator=gen, device="cuda").to(DT[at])
+    g = torch.randn(K, ld, generator=gen, device="cuda").to(DT[gt])
+    before = g.clone()
+    emb = B.Embedding(K, ld, gap, V, D, scale=0.75, max_tokens=T + 5)
+    emb.gradient(dy, t, g, accumulate=acc)
+    old = before[:, gap:gap + V * D].view(K, V, D) if acc else None
+    want, bound = gradient_reference(dy, t, V, 0.75, old)
+    got = g[:, gap:gap + V * D].view(K, V, D)
+    err = (got.double() - want).abs()
+    assert bool((err <= bound + half_ulp(want.abs() + bound, DT[gt])).all()), float((err - bound).max())
+    # nothing outside the table's slice, and no row that no token selects when adding
+    if gap:
+        assert torch.equal(g[:, :gap], before[:, :gap]) and torch.equal(g[:, gap + V * D:], before[:, gap + V * D:])
+    if T:
+        met = torch.zeros(K, V, dtype=torch.bool, device="cuda")
+        for k in range(K):
+            met[k, t[k][valid(t[k], V)].long()] = True
+        same = got[~met]
+        assert torch.equal(same, (old if acc else torch.zeros_like(got))[~met])
+    # equal inputs give equal bits
+    again = before.clone()
+    emb.gradient(dy, t, again, accumulate=acc)
+    assert torch.equal(again, g)
+
+
+def test_gradient_of_views_that_are_not_16_byte_aligned():
+    from paper_2006_00441_b200 import binding as B
+    K, T, V, D = 2, 100, 50, 64
+    gen, tok, ld = make(K, T, V, D, 0)
+    flat = torch.randn(K * T * D + 1, generator=gen, device="cuda")
+    gflat = torch.zeros(K * ld + 1, device="cuda")
+    dy, g = flat[1:].view(K, T, D), gflat[1:].view(K, ld)
+    emb = B.Embedding(K, ld, 0, V, D, max_tokens=T)
+    emb.gradient(dy, tok, g)
+    want, bound = gradient_reference(dy, tok, V, 1.0, None)
+    assert bool(((g.view(K, V, D).double() - want).abs() <= bound).all()) and float(gflat[0]) == 0.0
+    out = emb.lookup(g, tok)
+    ok = valid(tok, V)
+    assert torch.equal(out[ok], torch.stack([g.view(K, V, D)[k, tok[k].where(ok[k], 0)] for k in range(K)])[ok])
+
+
+def test_gradient_is_the_lookups_adjoint_and_its_difference_quotient():
+    """f(E) = <dy, lookup(E)> is linear in E, so <gradient(dy), H> = (f(E + H) - f(E)) for every H: in float32, up to the
+    rounding of the two lookups (u of each element) and of the gradient's sums."""
+    from paper_2006_00441_b200 import binding as B
+    K, T, V, D = 2, 600, 90, 48
+    gen, tok, ld = make(K, T, V, D, 4, pad=0.2)
+    E, H = (torch.randn(K, ld, generator=gen, device="cuda") for _ in range(2))
+    dy = torch.randn(K, T, D, generator=gen, device="cuda")
+    emb = B.Embedding(K, ld, 4, V, D, scale=1.5, max_tokens=T)
+    g = torch.zeros(K, ld, device="cuda")
+    emb.gradient(dy, tok, g)
+    EH = E + H
+    f1, f0 = emb.lookup(EH, tok).double(), emb.lookup(E, tok).double()
+    lhs = (g.double() * (EH.double() - E.double())).sum()
+    rhs = (dy.double() * (f1 - f0)).sum()
+    _, bound = gradient_reference(dy, tok, V, 1.5, None)
+    slack = U * (dy.double().abs() * (f1.abs() + f0.abs())).sum() + (bound * (EH - E)[:, 4:4 + V * D].view(K, V, D).double().abs()).sum()
+    assert abs(float(lhs - rhs)) <= float(slack)
+
+
+def test_calls_on_different_streams_share_the_workspace_safely():
+    from paper_2006_00441_b200 import binding as B
+    K, T, V, D = 2, 4000, 500, 256
+    emb = B.Embedding(K, V * D, 0, V, D, max_tokens=T)
+    jobs = []
+    torch.cuda.synchronize()
+    for i in range(6):
+        gen, tok, ld = make(K, T, V, D, 0, seed=i)
+        dy = torch.randn(K, T, D, generator=gen, device="cuda")
+        jobs.append((dy, tok, torch.zeros(K, ld, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for dy, tok, g, s in jobs:
+        with torch.cuda.stream(s):
+            emb.gradient(dy, tok, g)
+    torch.cuda.synchronize()
+    for dy, tok, g, _ in jobs:
+        want, bound = gradient_reference(dy, tok, V, 1.0, None)
+        assert bool(((g.view(K, V, D).double() - want).abs() <= bound).all())
+
+
+def test_a_gradient_array_beyond_two_to_the_31_elements():
+    """Offsets past 32 bits: the second replica's table lies beyond element 2^31 of the array."""
+    from paper_2006_00441_b200 import binding as B
+    V, D = 40, 64
+    ld = 2 ** 31 + 64
+    gap = ld - V * D
+    g = torch.zeros(2, ld, dtype=torch.bfloat16, device="cuda")
+    tok = torch.randint(0, V, (2, 200), device="cuda")
+    dy = torch.randn(2, 200, D, device="cuda").bfloat16()
+    emb = B.Embedding(2, ld, gap, V, D, max_tokens=200)
+    emb.gradient(dy, tok, g)
+    want, bound = gradient_reference(dy, tok, V, 1.0, None)
+    got = g[:, gap:].view(2, V, D).double()
+    assert bool(((got - want).abs() <= bound + half_ulp(want.abs() + bound, torch.bfloat16)).all())
+    assert torch.equal(emb.lookup(g, tok)[1], g[1, gap:].view(V, D)[tok[1]])
+
+
+def test_wrapper_refuses_what_it_cannot_take():
+    from paper_2006_00441_b200 import binding as B
+    emb = B.Embedding(2, 64, 0, 8, 8, max_tokens=4)
+    w, tok = torch.zeros(2, 64, device="cuda"), torch.zeros(2, 4, dtype=torch.int64, device="cuda")
+    dy = torch.zeros(2, 4, 8, device="cuda")
+    for bad in (lambda: emb.lookup(w.half(), tok), lambda: emb.lookup(w[:1], tok), lambda: emb.lookup(w, tok.to(torch.int16)),
+                lambda: emb.lookup(w, tok.cpu()), lambda: emb.lookup(w, tok.T), lambda: emb.lookup(w, tok, out_dtype=torch.float16),
+                lambda: emb.lookup(w, tok, out=dy[:, :2]), lambda: emb.gradient(dy[:, :3], tok, w),
+                lambda: emb.gradient(torch.zeros(2, 5, 8, device="cuda"), torch.zeros(2, 5, dtype=torch.int64, device="cuda"), w)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(B.DasgdError):
+        B.Embedding(2, 63, 0, 8, 8)

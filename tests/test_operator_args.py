@@ -1,0 +1,74 @@
+"""The operators of language-model replicas refuse bad arguments before they touch CUDA (no GPU needed)."""
+import ctypes
+
+import pytest
+
+from paper_2006_00441_b200 import binding as B
+
+
+def _embed(**kw):
+    c = B.dasgd_embed_config()
+    c.K, c.V, c.D, c.device, c.T, c.ld, c.offset, c.scale, c.token_bits = 2, 10, 8, 0, 5, 100, 4, 1.0, 64
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+@pytest.mark.parametrize("bad,frag", [
+    (dict(K=0), "K must"), (dict(K=65536), "K must"), (dict(V=0), "V must"), (dict(D=0), "D must"), (dict(T=-1), "T must"), (dict(T=2 ** 31), "T must"),
+    (dict(ld=83), "inside a row"), (dict(offset=-1), "inside a row"), (dict(offset=21), "inside a row"), (dict(token_bits=16), "token_bits"),
+    (dict(table_elem=2), "element type"), (dict(rows_elem=-1), "element type"), (dict(device=-1), "device"),
+])
+def test_embedding_configuration_is_checked(bad, frag):
+    c = _embed(**bad)
+    for call in (lambda: B.dasgd_embed_workspace(c), lambda: B.dasgd_embed_lookup(c, 0x1000, 0x1000, 0x1000, None),
+                 lambda: B.dasgd_embed_gradient(c, 0x1000, 0x1000, 0x1000, 0x1000, 1 << 30, None)):
+        with pytest.raises(B.DasgdError) as e:
+            call()
+        assert e.value.status == B.DASGD_ERR_INVALID_ARG and frag in str(e.value)
+
+
+def test_embedding_pointers_and_workspace_are_checked():
+    c = _embed()
+    n = B.dasgd_embed_workspace(c)
+    for args, frag in [((None, 0x1000, 0x1000), "NULL"), ((0x1000, None, 0x1000), "NULL"), ((0x1000, 0x1000, None), "NULL"),
+                       ((0x1002, 0x1000, 0x1000), "aligned"), ((0x1000, 0x1004, 0x1000), "aligned"), ((0x1000, 0x1000, 0x1001), "aligned")]:
+        with pytest.raises(B.DasgdError) as e:
+            B.dasgd_embed_lookup(c, *args, None)
+        assert frag in str(e.value)
+    for args, frag in [((None, 0x1000, 0x1000, 0x1000, n), "NULL"), ((0x1000, 0x1000, 0x1000, None, n), "workspace"),
+                       ((0x1000, 0x1000, 0x1000, 0x1000, n - 1), "workspace"), ((0x1000, 0x1000, 0x1000, 0x1010, n), "workspace"),
+                       ((0x1001, 0x1000, 0x1000, 0x1000, n), "aligned")]:
+        with pytest.raises(B.DasgdError) as e:
+            B.dasgd_embed_gradient(c, *args, None)
+        assert e.value.status == B.DASGD_ERR_INVALID_ARG and frag in str(e.value)
+    assert B._L.dasgd_embed_lookup(None, None, None, None, None) == B.DASGD_ERR_INVALID_ARG
+    assert B._L.dasgd_embed_workspace(ctypes.byref(c), None) == B.DASGD_ERR_INVALID_ARG
+
+
+def test_embedding_calls_without_tokens_do_nothing():
+    c = _embed(T=0, accumulate=1)
+    B.dasgd_embed_lookup(c, None, None, None, None)
+    B.dasgd_embed_gradient(c, None, None, None, None, 0, None)
+
+
+@pytest.mark.parametrize("K,V,D", [(1, 10, 8), (3, 50000, 1024), (8, 259, 333)])
+def test_embedding_workspace_serves_fewer_tokens(K, V, D):
+    sizes = [B.dasgd_embed_workspace(_embed(K=K, V=V, D=D, T=T, ld=V * D + 8)) for T in sorted({0, 1, 31, 32, 33, 1000, 4096, 20000, 65536, 65537, 200000})]
+    assert sizes == sorted(sizes)
+
+
+def test_embedding_config_layout_matches_the_binding(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    for name, mirror in [("dasgd_embed_config", B.dasgd_embed_config)]:
+        fields = [f[0] for f in mirror._fields_]
+        src = tmp_path / f"{name}.c"
+        src.write_text('#include "dasgd.h"\n#include <stddef.h>\n#include <stdio.h>\nint main(void) {\n'
+                       + "\n".join(f'  printf("{f} %zu\\n", offsetof({name}, {f}));' for f in fields)
+                       + f'\n  printf("sizeof %zu\\n", sizeof({name}));\n  return 0;\n}}\n')
+        exe = tmp_path / name
+        subprocess.run(["gcc", "-std=c99", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
+        out = dict(line.split() for line in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.splitlines())
+        assert all(int(out[f]) == getattr(mirror, f).offset for f in fields) and int(out["sizeof"]) == ctypes.sizeof(mirror)
