@@ -374,6 +374,46 @@ dasgd_status dasgd_embed_workspace(const dasgd_embed_config *cfg, int64_t *bytes
 dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy_device, const void *tokens_device,
                                   void *grad_array_device, void *workspace_device, int64_t workspace_bytes, void *stream);
 
+/* Directions of a local step for weight matrices: momentum, then Newton-Schulz steps that carry the singular values of
+ * each matrix toward 1 ("orthogonalised" update).  For every replica k and matrix i, elementwise in float32:
+ *     m <- momentum*m + g;   u = nesterov ? g + momentum*m : m           (momentum = 0: u = g, m is NULL)
+ *     X = u / (|u|_F + eps);   steps times:  X <- a*X + (b*A + c*A*A)*X,  A = X*X^T  (X^T*X from the right if rows > cols)
+ *     out = scale_i * X
+ * Only the matrices' slices of m and out are written; out may be g.  With out = the gradient array (in place),
+ * dasgd_step of a context with momentum 0 then subtracts lr*out, snapshots and merges as for any gradient.
+ * Products run on the tensor cores: cfg.dtype DASGD_BF16_MASTER_F32 (g, out bfloat16) multiplies fp16 operands,
+ * DASGD_F32 (g, out float32) pairs of fp16 numbers; sums are float32.  Equal inputs give equal bits. */
+typedef struct {
+  int64_t offset;        /* first element of the matrix in each row of the arrays */
+  int32_t rows, cols;    /* row-major, contiguous, 1 .. 2^20; matrices must not overlap */
+  float scale;
+} dasgd_matrix;
+
+typedef struct {
+  int32_t K, n_matrices;
+  int32_t dtype;               /* dasgd_dtype: the type of g and out                                              */
+  int32_t steps;               /* 1 .. 16; 0 = 5                                                                  */
+  int32_t nesterov, device;
+  int32_t tile;                /* 0 = by size; 128 or 256: side of the tiles that the products are computed in    */
+  uint32_t timeout_ms;         /* limit of every wait inside the kernel; 0 = 10000                                */
+  int64_t ld;                  /* row stride of g, m and out, elements                                            */
+  float momentum, eps;
+  const dasgd_matrix *matrices;   /* host, [n_matrices]; not needed after the call                                 */
+  const float *coefficients;      /* host, [steps][3] = a, b, c; NULL = 3.4445, -4.7750, 2.0315 in every step.
+                                     DASGD_ERR_UNSUPPORTED if they could carry an entry past fp16's range         */
+  void *workspace;                /* device, 256-byte aligned, kept by the caller until dasgd_ortho_destroy       */
+  int64_t workspace_bytes;
+} dasgd_ortho_config;
+
+typedef struct dasgd_ortho dasgd_ortho;
+dasgd_status dasgd_ortho_workspace(const dasgd_ortho_config *cfg, int64_t *bytes); /* ignores cfg->workspace */
+dasgd_status dasgd_ortho_init(dasgd_ortho **op, const dasgd_ortho_config *cfg, void *stream); /* waits for stream */
+/* Calls of one operator share its workspace: calls that can overlap on the GPU must be ordered by the caller. */
+dasgd_status dasgd_ortho_step(dasgd_ortho *op, const void *g_device, float *m_device, void *out_device, void *stream);
+/* Waits for the stream; DASGD_ERR_TIMEOUT if a wait inside a kernel since the last call ran past timeout_ms. */
+dasgd_status dasgd_ortho_sync(dasgd_ortho *op, void *stream);
+dasgd_status dasgd_ortho_destroy(dasgd_ortho *op); /* does not wait: synchronise first */
+
 /* Library version, "major.minor". */
 const char *dasgd_version(void);
 

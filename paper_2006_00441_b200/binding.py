@@ -40,6 +40,7 @@ EXPORTS = [
     "dasgd_get_kernel_units", "dasgd_refresh_lp",
     "dasgd_set_momentum_averaging", "dasgd_get_pending_momentum",
     "dasgd_embed_lookup", "dasgd_embed_workspace", "dasgd_embed_gradient",
+    "dasgd_ortho_workspace", "dasgd_ortho_init", "dasgd_ortho_step", "dasgd_ortho_sync", "dasgd_ortho_destroy",
     "dasgd_set_shard", "dasgd_set_shard_nccl", "dasgd_nccl_unique_id", "dasgd_nccl_comm_init", "dasgd_nccl_comm_destroy",
 ]
 
@@ -66,6 +67,20 @@ class dasgd_embed_config(ctypes.Structure):
         ("T", ctypes.c_int64), ("ld", ctypes.c_int64), ("offset", ctypes.c_int64),
         ("scale", ctypes.c_float), ("token_bits", ctypes.c_int32), ("table_elem", ctypes.c_int32),
         ("rows_elem", ctypes.c_int32), ("accumulate", ctypes.c_int32),
+    ]
+
+
+class dasgd_matrix(ctypes.Structure):
+    _fields_ = [("offset", ctypes.c_int64), ("rows", ctypes.c_int32), ("cols", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class dasgd_ortho_config(ctypes.Structure):
+    _fields_ = [
+        ("K", ctypes.c_int32), ("n_matrices", ctypes.c_int32), ("dtype", ctypes.c_int32), ("steps", ctypes.c_int32),
+        ("nesterov", ctypes.c_int32), ("device", ctypes.c_int32), ("tile", ctypes.c_int32), ("timeout_ms", ctypes.c_uint32),
+        ("ld", ctypes.c_int64), ("momentum", ctypes.c_float), ("eps", ctypes.c_float),
+        ("matrices", ctypes.POINTER(dasgd_matrix)), ("coefficients", ctypes.POINTER(ctypes.c_float)),
+        ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
     ]
 
 
@@ -121,6 +136,12 @@ def _load() -> ctypes.CDLL:
     L.dasgd_embed_lookup.argtypes = [pemb, vp, vp, vp, vp]
     L.dasgd_embed_workspace.argtypes = [pemb, ctypes.POINTER(i64)]
     L.dasgd_embed_gradient.argtypes = [pemb, vp, vp, vp, vp, i64, vp]
+    port = ctypes.POINTER(dasgd_ortho_config)
+    L.dasgd_ortho_workspace.argtypes = [port, ctypes.POINTER(i64)]
+    L.dasgd_ortho_init.argtypes = [ctypes.POINTER(vp), port, vp]
+    L.dasgd_ortho_step.argtypes = [vp, vp, vp, vp, vp]
+    L.dasgd_ortho_sync.argtypes = [vp, vp]
+    L.dasgd_ortho_destroy.argtypes = [vp]
     L.dasgd_version.argtypes = []
     L.dasgd_version.restype = ctypes.c_char_p
     return L
@@ -322,6 +343,30 @@ def dasgd_embed_gradient(cfg: dasgd_embed_config, dy_ptr: int, tokens_ptr: int, 
                                    stream_ptr), None)
 
 
+def dasgd_ortho_workspace(cfg: dasgd_ortho_config) -> int:
+    n = ctypes.c_int64()
+    _check(_L.dasgd_ortho_workspace(ctypes.byref(cfg), ctypes.byref(n)), None)
+    return n.value
+
+
+def dasgd_ortho_init(cfg: dasgd_ortho_config, stream_ptr: int | None) -> ctypes.c_void_p:
+    op = ctypes.c_void_p()
+    _check(_L.dasgd_ortho_init(ctypes.byref(op), ctypes.byref(cfg), stream_ptr), None)
+    return op
+
+
+def dasgd_ortho_step(op, g_ptr: int, m_ptr: int | None, out_ptr: int, stream_ptr: int | None):
+    _check(_L.dasgd_ortho_step(op, g_ptr, m_ptr, out_ptr, stream_ptr), None)
+
+
+def dasgd_ortho_sync(op, stream_ptr: int | None):
+    _check(_L.dasgd_ortho_sync(op, stream_ptr), None)
+
+
+def dasgd_ortho_destroy(op):
+    _check(_L.dasgd_ortho_destroy(op), None)
+
+
 _ELEM = {torch.float32: DASGD_ELEM_F32, torch.bfloat16: DASGD_ELEM_BF16}
 _TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
 
@@ -403,6 +448,71 @@ class Embedding:
         dasgd_embed_gradient(self.cfg, dy.data_ptr(), tokens.data_ptr(), g.data_ptr(), self._ws.data_ptr(),
                              self._ws.numel(), stream)
         return g
+
+
+class Ortho:
+    """Orthogonalised directions for weight matrices of K replicas (momentum, then Newton-Schulz steps).
+
+    ``matrices``: ``(offset, rows, cols)`` or ``(offset, rows, cols, scale)`` for each matrix, a contiguous row-major slice of
+    every row of the ``[K, ld]`` arrays.  ``dtype`` is the engine's: gradients and directions are float32 (DASGD_F32) or
+    bfloat16 (DASGD_BF16_MASTER_F32), the momentum array float32.  ``coefficients``: one ``(a, b, c)`` for all steps, or one
+    for each.  Calls are enqueued on torch's current stream of ``device`` and return at once.
+    """
+
+    def __init__(self, K, ld, matrices, dtype=DASGD_F32, momentum=0.95, nesterov=True, steps=5, coefficients=None, eps=1e-7,
+                 device=0, tile=0, timeout_ms=0):
+        if not torch.cuda.is_available():
+            raise RuntimeError("Ortho needs a CUDA device; there is no CPU implementation")
+        self.op = None
+        self.K, self.ld, self.momentum = K, ld, momentum
+        self.device = torch.device("cuda", device)
+        self.gdtype = torch.bfloat16 if dtype == DASGD_BF16_MASTER_F32 else torch.float32
+        c = dasgd_ortho_config()
+        c.K, c.n_matrices, c.dtype, c.steps, c.device, c.ld = K, len(matrices), dtype, steps, device, ld
+        c.momentum, c.nesterov, c.eps, c.tile, c.timeout_ms = momentum, int(nesterov and momentum != 0), eps, tile, timeout_ms
+        c.matrices = (dasgd_matrix * len(matrices))(*(dasgd_matrix(*m, *((1.0,) if len(m) == 3 else ())) for m in matrices))
+        if coefficients is not None:
+            flat = list(coefficients)
+            flat = [float(v) for row in flat for v in row] if hasattr(flat[0], "__len__") else [float(v) for v in flat] * steps
+            if len(flat) != 3 * steps:
+                raise ValueError(f"coefficients must be (a, b, c) or {steps} of them")
+            c.coefficients = (ctypes.c_float * len(flat))(*flat)
+        n = dasgd_ortho_workspace(c)
+        self._order = _StreamOrder(self.device)
+        self._ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        c.workspace, c.workspace_bytes = self._ws.data_ptr(), n
+        self.op = dasgd_ortho_init(c, torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _ptr(self, t, dtype, what):
+        if t.dtype != dtype or tuple(t.shape) != (self.K, self.ld) or not t.is_contiguous() or t.device != self.device:
+            raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {(self.K, self.ld)} on {self.device}")
+        return t.data_ptr()
+
+    def step(self, g, m=None, out=None):
+        """Updates ``m`` and writes the matrices' slices of ``out`` (default: ``g`` itself); the rest of ``out`` stays."""
+        out = g if out is None else out
+        if (m is None) != (self.momentum == 0):
+            raise ValueError("m must be given exactly when momentum != 0")
+        gp, op = self._ptr(g, self.gdtype, "g"), self._ptr(out, self.gdtype, "out")
+        mp = self._ptr(m, torch.float32, "m") if m is not None else None
+        dasgd_ortho_step(self.op, gp, mp, op, self._order.enter((self._ws,)))
+        return out
+
+    def sync(self):
+        """Waits for the last call; raises if a wait inside the kernel ran out of time."""
+        dasgd_ortho_sync(self.op, self._order.last.cuda_stream)
+
+    def close(self):
+        if getattr(self, "op", None):
+            self._order.last.synchronize()
+            dasgd_ortho_destroy(self.op)
+            self.op = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # ---------------------------------------------------------------- convenience wrapper

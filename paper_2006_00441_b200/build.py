@@ -14,7 +14,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libdasgd.so")
 SOURCES = [os.path.join(CSRC, "dasgd_api.cu"), os.path.join(CSRC, "dasgd_noalloc.cu"), os.path.join(CSRC, "dasgd_nccl.cu"),
-           os.path.join(CSRC, "dasgd_embed.cu")]
+           os.path.join(CSRC, "dasgd_embed.cu"), os.path.join(CSRC, "dasgd_ortho.cu")]
 HEADERS = [os.path.join(CSRC, "dasgd_kernels.cuh"), os.path.join(ROOT, "include", "dasgd.h")]
 
 

@@ -1,0 +1,1125 @@
+// Orthogonalised directions for the weight matrices of K replicas: momentum, then Newton-Schulz steps.
+//
+//   m <- mu*m + g;   u = g + mu*m (Nesterov) or m;   X_0 = u / (|u|_F + eps)
+//   X_{t+1} = a X_t + (b A + c A^2) X_t,   A = X_t X_t^T            (on the smaller side; X_t^T X_t on the right otherwise)
+//   out = scale * X_steps
+//
+// With n <= w the two sides of a matrix, a step costs n^2 w + n^3 + 2 n^2 w operations (A and A^2 are symmetric: only
+// tiles on and above the diagonal are computed; a tile below it is read as the transpose of its mirror image).
+//
+// Numbers.  The products run on the tensor cores with fp16 operands and float32 accumulators.  An iteration multiplies
+// small singular values by a > 3 and leaves large ones where they are, so a rounding error made early grows with the
+// weakest directions; rounding X, A or B = bA + cA^2 to 11 bits and multiplying the results through loses several per cent
+// on a matrix with a decaying spectrum.  Therefore
+//   - the iterate X is kept as a pair of fp16 numbers (22 bits), and the term a X is taken from the pair;
+//   - the diagonals of A and B, their largest entries, are kept in float32 and applied in the epilogues:
+//       A = D + O:  A^2_ij = (O^2)_ij + O_ij (D_i + D_j), A^2_ii = (O^2)_ii + D_i^2;   BX = diag(B) X + off(B) X;
+//   - only off-diagonal parts and the leading half of X enter products ("half" operands, for bfloat16 directions).  Their
+//     errors stay below the rounding of the output (2-norm, against 64 bits: 2e-4 to 1.3e-3, the rounding being 1.7e-3);
+//   - for float32 directions every operand is a pair and every product three (hi hi + hi lo + lo hi).
+// Everything in fp16 is stored times 2^12, so that pairs of entries of size 1/4096 stay clear of the subnormals; the host
+// refuses coefficients that could carry an entry past the largest fp16 number.
+#include "dasgd.h"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+#include <string>
+#include <type_traits>
+#include <utility>
+#include <vector>
+
+extern "C" __attribute__((visibility("hidden"))) dasgd_status dasgd_internal_fail(dasgd_ctx *ctx, dasgd_status st, const char *msg);
+
+namespace {
+
+constexpr int kMaxSteps = 16;
+constexpr float kStore = 4096.f;                          // what an fp16 entry is stored times
+constexpr float kUnstore = 1.f / kStore, kUnstore2 = kUnstore * kUnstore;
+constexpr double kMaxEntry = 15.0;                        // * kStore < 65504
+
+constexpr int kBox = 64;                                  // TMA box: 64 x 64 fp16, 8 KB, rows of 128 bytes
+constexpr int kBoxBytes = kBox * kBox * 2;
+constexpr int kSlotBytes = 4 * kBoxBytes;                 // 128 x 64 of either operand
+constexpr int kSlots = 6;
+constexpr int kEpiWarps = 8, kThreads = 128 + kEpiWarps * 32;
+constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;    // + slack to start on a 1024-byte boundary
+
+enum { GRAM = 0, SQUARE = 1, UPDATE = 2 };
+enum { MAP_X = 0, MAP_A = 4, MAP_B = 6, MAPS = 8 };       // MAP_X + 2 * buffer + part; MAP_A + part; MAP_B + part
+
+struct Group {                                            // matrices of one shape, all replicas
+  int rows, cols, n, w, flip;                             // n = the smaller side; flip: n is the columns
+  int matrices, batch;                                    // batch = matrices * K, index z = matrix * K + replica
+  int tn, tw, tg, tu;                                     // tiles of the sides; tiles of a symmetric product, of an update
+  int even;                                               // 1: every matrix starts on a multiple of 8 elements of a row; 2: and has rows of such lengths
+  int ldx, lda;                                           // row strides (elements) of X and of A, B
+  int z0, m0;                                             // first matrix-of-a-replica, first matrix, over all groups
+  int chunks, chunk0;                                     // pieces of a matrix in the momentum kernel; first piece of the group
+  int rblk, rblks, rblk0;                                 // rows of a piece, pieces, first piece in the scaling kernel
+  __half *x[2][2], *a[2], *b[2];                          // [buffer][part], [part]
+  float *da, *db;                                         // diagonals of A and B, [batch][lda]
+};
+
+struct Plan {                                             // kernel argument
+  const Group *groups;
+  const CUtensorMap *maps;                                // [groups][MAPS]
+  const long long *offset;                                // [matrices]
+  const float *scale;                                     // [matrices]
+  unsigned *done;                                         // [matrices * K] epilogue warps that have finished a tile
+  double *sumsq;                                          // [pieces] of the momentum kernel
+  int *error;
+  int n_groups, K, steps, n_done;
+  long long ld;
+  float coef[kMaxSteps][3];
+  float mu, eps;
+  int nesterov;
+  unsigned long long timeout_ns;
+};
+
+// ---------------------------------------------------------------- momentum and norm
+
+constexpr int kPrepThreads = 256, kChunk = 16384;
+
+template <typename T>
+__device__ __forceinline__ float to_f(T v) { return static_cast<float>(v); }
+
+template <typename T>
+__device__ __forceinline__ void load8(const T *p, float (&x)[8]) {
+  if constexpr (sizeof(T) == 4) {
+    const float4 a = *reinterpret_cast<const float4 *>(p), b = *(reinterpret_cast<const float4 *>(p) + 1);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  } else {
+    const uint4 v = *reinterpret_cast<const uint4 *>(p);
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(u[i] << 16), x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+  }
+}
+
+__device__ __forceinline__ float direction(float g, float m, float mu, int nesterov) { return nesterov ? fmaf(mu, m, g) : m; }
+
+__device__ __forceinline__ int group_of(const Plan &p, int at, int Group::*first) {
+  int g = 0;
+  while (g + 1 < p.n_groups && at >= p.groups[g + 1].*first) ++g;
+  return g;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kPrepThreads) k_ortho_momentum(const Plan p, const T *g, float *m, int vec) {
+  __shared__ double part[kPrepThreads / 32];
+  for (int i = blockIdx.x * kPrepThreads + threadIdx.x; i < p.n_done; i += gridDim.x * kPrepThreads) p.done[i] = 0;
+  const Group &gr = p.groups[group_of(p, blockIdx.x, &Group::chunk0)];
+  const int local = blockIdx.x - gr.chunk0, z = local / gr.chunks, c = local % gr.chunks;
+  const long long numel = (long long)gr.rows * gr.cols, lo = (long long)c * kChunk, hi = min(numel, lo + kChunk);
+  const long long base = (z % p.K) * p.ld + p.offset[gr.m0 + z / p.K];
+  const T *gp = g + base;
+  float *mp = m ? m + base : nullptr;
+  float s = 0.f;
+  long long e = lo;
+  if (vec && gr.even) {
+    for (e = lo + threadIdx.x * 8; e + 8 <= hi; e += kPrepThreads * 8) {
+      float x[8];
+      load8(gp + e, x);
+      if (mp) {
+        float o[8];
+        load8(mp + e, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = fmaf(p.mu, o[i], x[i]);
+        *reinterpret_cast<float4 *>(mp + e) = make_float4(o[0], o[1], o[2], o[3]);
+        *reinterpret_cast<float4 *>(mp + e + 4) = make_float4(o[4], o[5], o[6], o[7]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = direction(x[i], o[i], p.mu, p.nesterov);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+    }
+    e = lo + (hi - lo) / 8 * 8;
+  }
+  for (e += threadIdx.x; e < hi; e += kPrepThreads) {
+    float x = to_f(gp[e]);
+    if (mp) {
+      const float o = fmaf(p.mu, mp[e], x);
+      mp[e] = o;
+      x = direction(x, o, p.mu, p.nesterov);
+    }
+    s = fmaf(x, x, s);
+  }
+  double d = s;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = d;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kPrepThreads / 32; ++i) d += part[i];
+    p.sumsq[blockIdx.x] = d;
+  }
+}
+
+__device__ __forceinline__ uint32_t pack_half(__half a, __half b) {
+  return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16;
+}
+
+// X_0 as a pair of fp16, the padding of its rows zeroed.
+template <typename T>
+__global__ void __launch_bounds__(kPrepThreads) k_ortho_scale(const Plan p, const T *g, const float *m, int vec) {
+  __shared__ double part[kPrepThreads / 32];
+  const Group &gr = p.groups[group_of(p, blockIdx.x, &Group::rblk0)];
+  const int local = blockIdx.x - gr.rblk0, z = local / gr.rblks, r0 = local % gr.rblks * gr.rblk;
+  double d = 0.0;
+  for (int i = threadIdx.x; i < gr.chunks; i += kPrepThreads) d += p.sumsq[gr.chunk0 + z * gr.chunks + i];
+#pragma unroll
+  for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = d;
+  __syncthreads();
+  d = 0.0;
+  for (int i = 0; i < kPrepThreads / 32; ++i) d += part[i];
+  const float f = (float)((double)kStore / (sqrt(d) + (double)p.eps));
+
+  const long long base = (z % p.K) * p.ld + p.offset[gr.m0 + z / p.K];
+  const T *gp = g + base;
+  const float *mp = m ? m + base : nullptr;
+  const long long xbase = (long long)z * gr.rows * gr.ldx;
+  const int units = gr.ldx / 8, r1 = min(gr.rows, r0 + gr.rblk);
+  for (int i = threadIdx.x; i < (r1 - r0) * units; i += kPrepThreads) {
+    const int r = r0 + i / units, c = i % units * 8;
+    const long long at = (long long)r * gr.cols + c;
+    float x[8];
+    if (vec && gr.even == 2 && c + 8 <= gr.cols) {
+      load8(gp + at, x);
+      if (mp) {
+        float o[8];
+        load8(mp + at, o);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = direction(x[j], o[j], p.mu, p.nesterov);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] = 0.f;
+        if (c + j < gr.cols) {
+          x[j] = to_f(gp[at + j]);
+          if (mp) x[j] = direction(x[j], mp[at + j], p.mu, p.nesterov);
+        }
+      }
+    }
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float a = x[2 * j] * f, b = x[2 * j + 1] * f;
+      const __half ha = __float2half_rn(a), hb = __float2half_rn(b);
+      h[j] = pack_half(ha, hb);
+      l[j] = pack_half(__float2half_rn(a - __half2float(ha)), __float2half_rn(b - __half2float(hb)));
+    }
+    const long long o = xbase + (long long)r * gr.ldx + c;
+    *reinterpret_cast<uint4 *>(gr.x[0][0] + o) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4 *>(gr.x[0][1] + o) = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+// ---------------------------------------------------------------- PTX
+
+__device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+
+// the address, in the cluster's window, of what CTA `rank` has at this offset of its shared memory
+__device__ __forceinline__ uint32_t mapped(uint32_t addr, int rank) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  return a;
+}
+
+// arrives on the barrier at the same offset in CTA `rank` of the cluster
+__device__ __forceinline__ void mbar_arrive(uint32_t bar, int rank) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped(bar, rank)) : "memory");
+}
+
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+
+__device__ __forceinline__ unsigned load_acquire(const unsigned *p) {
+  unsigned v;
+  asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ void add_release(unsigned *p, unsigned v) {
+  asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z) {
+  if constexpr (CG == 1) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+  } else {  // the barrier may be the other CTA's of the pair
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+  }
+}
+
+template <int CG>
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  if constexpr (CG == 1)
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((int)add) : "memory");
+  else
+    asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((int)add) : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  if constexpr (CG == 1)
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  else
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, int cols) {
+  if constexpr (CG == 1) asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+  else asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+  if constexpr (CG == 1) asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  else asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+}
+
+template <int CG>
+__device__ __forceinline__ void tmem_free(uint32_t addr, int cols) {
+  if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+  else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+}
+
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
+      "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// Shared-memory matrix descriptors for 128-byte swizzled boxes.  Rows along the product's inner dimension ("inner"): 8 rows
+// of 128 bytes make an atom, atoms of further rows follow every 1024 bytes.  Rows along the outer dimension ("outer", a box
+// read as its transpose): the next 8 inner indices follow after 1024 bytes, the next 64 outer ones in the next box.
+constexpr uint64_t kDescBase = (1ull << 46) | (2ull << 61) | (uint64_t)(1024 >> 4) << 32;
+__device__ __forceinline__ uint64_t descriptor(uint32_t addr, bool outer) {
+  return kDescBase | (uint64_t)(outer ? kBoxBytes >> 4 : 1) << 16 | (addr >> 4 & 0x3fff);
+}
+__device__ __forceinline__ uint64_t desc_step(bool outer) { return outer ? 2048 >> 4 : 32 >> 4; }  // 16 inner indices
+
+// ---------------------------------------------------------------- the tiles, in the order in which they are taken
+
+// Steps, in each step the three products, in each product all matrices of all shapes, tile by tile: a tile depends only on
+// tiles before it, and with several matrices the ones it depends on were finished long ago.
+struct Tile {
+  int it, phase, z, ti, tj;
+  const Group *g;
+};
+
+template <int CG>
+struct Walk {
+  int it = 0, phase = 0, g = 0, seg0 = 0;
+  __device__ bool at(const Plan &p, int t, Tile &o) {
+    for (;;) {
+      if (it >= p.steps) return false;
+      const Group &gr = p.groups[g];
+      const int per = phase == UPDATE ? gr.tu : gr.tg, local = t - seg0;
+      if (local < per * gr.batch) {
+        o.it = it, o.phase = phase, o.g = &gr, o.z = local / per;
+        int r = local - o.z * per;
+        if (phase == UPDATE) {
+          const int tr = gr.flip ? gr.tw : gr.tn;
+          o.ti = r % tr, o.tj = r / tr;
+        } else {
+          int i = 0;
+          while (r >= gr.tn - i) r -= gr.tn - i, ++i;
+          o.ti = i, o.tj = i + r;
+        }
+        return true;
+      }
+      seg0 += per * gr.batch;
+      if (++g == p.n_groups) {
+        g = 0;
+        if (++phase == 3) phase = 0, ++it;
+      }
+    }
+  }
+};
+
+// finished epilogue warps of a matrix that a tile has to see: all tiles of the products before its own
+template <int CG>
+__device__ __forceinline__ unsigned needed(const Tile &t) {
+  return (unsigned)((t.it * (2 * t.g->tg + t.g->tu) + t.phase * t.g->tg) * CG * kEpiWarps);
+}
+
+struct Operand {   // one side of a product
+  int map;         // first of its maps (part 0)
+  int kind;        // 0: rows along the inner dimension; 1: rows along the outer one; 2: symmetric, tiles with row <= column stored
+  int t;           // its tile index along the outer dimension
+};
+
+template <int CG>
+__device__ __forceinline__ void operands(const Tile &t, Operand &a, Operand &b) {
+  const int xm = MAP_X + 2 * (t.it & 1), flip = t.g->flip;
+  if (t.phase == GRAM) a = {xm, flip, t.ti}, b = {xm, flip, t.tj};
+  else if (t.phase == SQUARE) a = {MAP_A, 2, t.ti}, b = {MAP_A, 2, t.tj};
+  else if (!flip) a = {MAP_B, 2, t.ti}, b = {xm, 1, t.tj};
+  else a = {xm, 0, t.ti}, b = {MAP_B, 2, t.tj};
+}
+
+template <int CG>
+__device__ __forceinline__ bool outer(const Operand &o, int kb) {  // whether the box of 64-wide inner block kb is read transposed
+  return o.kind == 1 || (o.kind == 2 && kb / (2 * CG) < o.t);
+}
+
+struct Shared {
+  uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2];
+  uint32_t tmem;
+  volatile int abort;
+};
+
+// Waits give up after the plan's time limit, or once another wait of this CTA has: the error word is set, all roles leave
+// their loops, and the CTA ends in order.
+struct Patience {
+  volatile int *abort;
+  int *error;
+  unsigned long long limit, since = 0;
+  __device__ bool over() {
+    if (*abort) return true;
+    const unsigned long long t = now_ns();
+    if (!since) since = t;
+    if (t - since < limit) return false;
+    *abort = 1;
+    atomicExch(error, 1);
+    return true;
+  }
+  __device__ bool bar(uint32_t b, uint32_t parity) {
+    since = 0;
+    for (int i = 1; !mbar_try(b, parity); ++i)
+      if ((i & 63) == 0 && over()) return false;
+    return true;
+  }
+  __device__ bool count(const unsigned *p, unsigned want) {  // want <= 2^31: counts never wrap
+    since = 0;
+    for (int i = 1; load_acquire(p) < want; ++i)
+      if ((i & 63) == 0 && over()) return false;
+    return true;
+  }
+};
+
+__device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8]) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&u[i]));
+    x[2 * i] = f.x, x[2 * i + 1] = f.y;
+  }
+}
+
+// 32 entries of a row, as fp16 and (where lo is not NULL) the rest as fp16 again
+__device__ __forceinline__ void store_pair(const float (&v)[32], __half *hi, __half *lo) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float a = v[8 * q + 2 * i], b = v[8 * q + 2 * i + 1];
+      const __half ha = __float2half_rn(a), hb = __float2half_rn(b);
+      h[i] = pack_half(ha, hb);
+      l[i] = pack_half(__float2half_rn(a - __half2float(ha)), __float2half_rn(b - __half2float(hb)));
+    }
+    *reinterpret_cast<uint4 *>(hi + 8 * q) = make_uint4(h[0], h[1], h[2], h[3]);
+    if (lo) *reinterpret_cast<uint4 *>(lo + 8 * q) = make_uint4(l[0], l[1], l[2], l[3]);
+  }
+}
+
+// 32 entries of a row of a stored pair (or of its leading half)
+__device__ __forceinline__ void load_pair(const __half *hi, const __half *lo, float (&v)[32]) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    float x[8];
+    unpack(__ldcg(reinterpret_cast<const uint4 *>(hi + 8 * q)), x);
+    if (lo) {
+      float y[8];
+      unpack(__ldcg(reinterpret_cast<const uint4 *>(lo + 8 * q)), y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] += y[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[8 * q + i] = x[i];
+  }
+}
+
+// One row's 32 columns of a finished tile.  row < the padded rows; stores are masked to the matrix.
+template <bool SPLIT, typename Out>
+__device__ __forceinline__ void finish(const Plan &p, const Tile &t, int row, int col, float (&acc)[32], Out *out, int vec) {
+  const Group &g = *t.g;
+  const int z = t.z;
+  const long long zd = (long long)z * g.lda;
+  if (t.phase != UPDATE) {
+    if (row >= g.lda || col >= g.lda) return;
+    const bool in = row < g.n, diag = t.ti == t.tj && (unsigned)(row - col) < 32u;
+    const long long at = ((long long)z * g.n + row) * g.lda + col;
+    float *d = t.phase == GRAM ? g.da : g.db;
+    if (t.phase == GRAM) {
+      if (diag) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+          if (col + i == row) d[zd + row] = acc[i] * kUnstore2, acc[i] = 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < 32; ++i) acc[i] *= kUnstore;
+      if (in) store_pair(acc, g.a[0] + at, SPLIT ? g.a[1] + at : nullptr);
+    } else {
+      const float b = p.coef[t.it][1], c = p.coef[t.it][2];
+      float o[32] = {};
+      if (in) load_pair(g.a[0] + at, SPLIT ? g.a[1] + at : nullptr, o);
+      const float di = __ldcg(g.da + zd + row);
+      const float4 *dj = reinterpret_cast<const float4 *>(g.da + zd + col);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        const float4 v = __ldcg(dj + q);
+        const float w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = 4 * q + i;
+          const float s = c * acc[e] * kUnstore;              // c (O^2)_ij, times kStore
+          if (diag && col + e == row) {
+            d[zd + row] = fmaf(di, fmaf(c, di, b), s * kUnstore);
+            acc[e] = 0.f;
+          } else {
+            acc[e] = fmaf(fmaf(c, di + w[i], b), o[e], s);
+          }
+        }
+      }
+      if (in) store_pair(acc, g.b[0] + at, SPLIT ? g.b[1] + at : nullptr);
+    }
+    return;
+  }
+  if (row >= g.rows || col >= g.ldx) return;
+  const float a = p.coef[t.it][0];
+  const long long at = ((long long)z * g.rows + row) * g.ldx + col;
+  const int cur = t.it & 1;
+  float x[32];
+  load_pair(g.x[cur][0] + at, g.x[cur][1] + at, x);
+  if (!g.flip) {
+    const float k = a + __ldcg(g.db + zd + row);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) acc[i] = fmaf(k, x[i], acc[i] * kUnstore);
+  } else {
+    const float4 *dj = reinterpret_cast<const float4 *>(g.db + zd + col);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const float4 v = __ldcg(dj + q);
+      acc[4 * q] = fmaf(a + v.x, x[4 * q], acc[4 * q] * kUnstore);
+      acc[4 * q + 1] = fmaf(a + v.y, x[4 * q + 1], acc[4 * q + 1] * kUnstore);
+      acc[4 * q + 2] = fmaf(a + v.z, x[4 * q + 2], acc[4 * q + 2] * kUnstore);
+      acc[4 * q + 3] = fmaf(a + v.w, x[4 * q + 3], acc[4 * q + 3] * kUnstore);
+    }
+  }
+  if (t.it + 1 < p.steps) {
+    store_pair(acc, g.x[cur ^ 1][0] + at, g.x[cur ^ 1][1] + at);
+    return;
+  }
+  const float s = p.scale[g.m0 + z / p.K] * kUnstore;
+  Out *o = out + (z % p.K) * p.ld + p.offset[g.m0 + z / p.K] + (long long)row * g.cols + col;
+  if (vec && g.even == 2 && col + 32 <= g.cols) {
+    if constexpr (sizeof(Out) == 4) {
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        reinterpret_cast<float4 *>(o)[q] = make_float4(acc[4 * q] * s, acc[4 * q + 1] * s, acc[4 * q + 2] * s, acc[4 * q + 3] * s);
+    } else {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(acc[8 * q + 2 * i] * s, acc[8 * q + 2 * i + 1] * s);
+          u[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        reinterpret_cast<uint4 *>(o)[q] = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+      if (col + i < g.cols) {
+        if constexpr (sizeof(Out) == 4) o[i] = acc[i] * s;
+        else o[i] = __float2bfloat16_rn(acc[i] * s);
+      }
+  }
+}
+
+// ---------------------------------------------------------------- all products of all steps in one launch
+
+// CG CTAs work on a tile of 128 CG x 128 CG.  Warp 0 loads, warp 1 multiplies, warps 4 to 11 finish tiles; two accumulators
+// in tensor memory let the next tile's products run while a tile is finished.  CTA (or pair) q takes tiles q, q + Q, ...:
+// every CTA is resident (cooperative launch) and tiles depend only on earlier ones, so the wait for them ends.
+template <int CG, bool SPLIT, typename Out>
+__global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *out, int vec) {
+  extern __shared__ uint8_t raw[];
+  __shared__ Shared sh;
+  constexpr int kCols = 128 * CG;
+  const uint32_t slots = (smem_u32(raw) + 1023) & ~1023u;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  int rank = 0;
+  if constexpr (CG == 2) asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
+  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&sh.full[i]), 1), mbar_init(smem_u32(&sh.empty[i]), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.acc_full[i]), 1), mbar_init(smem_u32(&sh.acc_empty[i]), CG * kEpiWarps);
+    sh.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 2) tmem_alloc<CG>(smem_u32(&sh.tmem), 2 * kCols);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if constexpr (CG == 2) cluster_barrier();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = sh.tmem;
+  Patience wait{&sh.abort, p.error, p.timeout_ns};
+  Walk<CG> walk;
+  Tile t;
+  constexpr int kParts = SPLIT ? 2 : 1;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int slot = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = first; ok && walk.at(p, i, t); i += stride) {
+        if (!(ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)))) break;
+        fence_async();
+        Operand oa, ob;
+        operands<CG>(t, oa, ob);
+        const CUtensorMap *maps = p.maps + (t.g - p.groups) * MAPS;
+        const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+        const int a0 = oa.t * kCols + rank * 128, b0 = ob.t * kCols + rank * 128;
+        for (int kb = 0; ok && kb < kbs; ++kb) {
+          const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {
+            if (!(ok = wait.bar(smem_u32(&sh.empty[slot]), phase ^ 1))) break;
+            uint32_t full = smem_u32(&sh.full[slot]);
+            if (rank == 0) mbar_expect(full, CG * kSlotBytes);
+            if constexpr (CG == 2) full = mapped(full, 0);
+            const uint32_t dst = slots + slot * kSlotBytes;
+            const CUtensorMap *ma = maps + oa.map + part, *mb = maps + ob.map + part;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              if (at) tma_load<CG>(dst + h * kBoxBytes, ma, full, a0 + h * kBox, kb * kBox, t.z);
+              else tma_load<CG>(dst + h * kBoxBytes, ma, full, kb * kBox, a0 + h * kBox, t.z);
+              if (bt) tma_load<CG>(dst + (2 + h) * kBoxBytes, mb, full, b0 + h * kBox, kb * kBox, t.z);
+              else tma_load<CG>(dst + (2 + h) * kBoxBytes, mb, full, kb * kBox, b0 + h * kBox, t.z);
+            }
+            if (++slot == kSlots) slot = 0, phase ^= 1;
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      int slot = 0, n = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      // float32 accumulators, fp16 operands, M = 128 CG, N = 128 CG
+      const uint32_t shape = 1u << 4 | (uint32_t)(kCols >> 3) << 17 | (uint32_t)(kCols >> 4) << 24;
+      for (int i = first; ok && walk.at(p, i, t); i += stride, ++n) {
+        const int acc = n & 1;
+        if (!(ok = wait.bar(smem_u32(&sh.acc_empty[acc]), (n >> 1 & 1) ^ 1))) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem + acc * kCols;
+        Operand oa, ob;
+        operands<CG>(t, oa, ob);
+        const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+        for (int kb = 0; ok && kb < kbs; ++kb) {
+          const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
+          const uint32_t idesc = shape | (uint32_t)at << 15 | (uint32_t)bt << 16;
+          const uint64_t sa = desc_step(at), sb = desc_step(bt);
+          uint64_t da[kParts], db[kParts];
+          int used[kParts];
+#pragma unroll
+          for (int part = 0; part < kParts; ++part) {
+            if (!(ok = wait.bar(smem_u32(&sh.full[slot]), phase))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t src = slots + slot * kSlotBytes;
+            da[part] = descriptor(src, at), db[part] = descriptor(src + 2 * kBoxBytes, bt), used[part] = slot;
+            if (part == 0) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[0] + k * sb, idesc, kb || k);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[kParts - 1] + k * sb, idesc, true);
+#pragma unroll
+              for (int k = 0; k < 4; ++k) mma<CG>(d, da[kParts - 1] + k * sa, db[0] + k * sb, idesc, true);
+            }
+            if (++slot == kSlots) slot = 0, phase ^= 1;
+          }
+          if (ok) {
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) mma_commit<CG>(smem_u32(&sh.empty[used[part]]));
+          }
+        }
+        if (ok) mma_commit<CG>(smem_u32(&sh.acc_full[acc]));
+      }
+    }
+  } else if (warp >= 4) {
+    const int q = warp & 3, half = (warp - 4) >> 2;
+    int n = 0;
+    for (int i = first; walk.at(p, i, t); i += stride, ++n) {
+      const int acc = n & 1;
+      // what the epilogue itself reads was finished by other CTAs: lane 0 acquires it for the warp
+      bool ok = true;
+      if (lane == 0) ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)) && wait.bar(smem_u32(&sh.acc_full[acc]), n >> 1 & 1);
+      if (!__shfl_sync(0xffffffffu, ok, 0)) break;
+      __syncwarp();
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      const int row = t.ti * kCols + rank * 128 + q * 32 + lane;
+#pragma unroll 1
+      for (int c = half * (kCols / 2); c < (half + 1) * (kCols / 2); c += 32) {
+        float v[32];
+        __syncwarp();
+        tmem_load32(tmem + ((uint32_t)(q * 32) << 16) + acc * kCols + c, v);
+        finish<SPLIT, Out>(p, t, row, t.tj * kCols + c, v, out, vec);
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      fence_async();  // the stores above are read by bulk copies
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(smem_u32(&sh.acc_empty[acc]), 0);
+        add_release(p.done + t.g->z0 + t.z, 1);
+      }
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (sh.abort) {  // copies and products may be in flight: they wait for nothing, so they end within this time
+    for (int i = 0; i < 200; ++i) __nanosleep(10000);
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if constexpr (CG == 2) cluster_barrier();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 2) tmem_free<CG>(tmem, 2 * kCols);
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- host side
+
+struct dasgd_ortho {
+  Plan plan{};
+  int device = 0, dtype = 0, cg = 1;
+  int chunks = 0, rblks = 0;
+  bool has_momentum = false;
+  int grid = 0;
+};
+
+namespace {
+
+dasgd_status bad(const std::string &m) { return dasgd_internal_fail(nullptr, DASGD_ERR_INVALID_ARG, m.c_str()); }
+dasgd_status unsupported(const std::string &m) { return dasgd_internal_fail(nullptr, DASGD_ERR_UNSUPPORTED, m.c_str()); }
+dasgd_status cuda_fail(cudaError_t e, const char *what) {
+  return dasgd_internal_fail(nullptr, DASGD_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
+}
+
+struct OnDevice {
+  int prev = -1;
+  cudaError_t e;
+  bool switched = false;
+  explicit OnDevice(int dev) {
+    e = cudaGetDevice(&prev);
+    if (e == cudaSuccess && prev != dev) {
+      e = cudaSetDevice(dev);
+      switched = e == cudaSuccess;
+    }
+  }
+  ~OnDevice() {
+    if (switched) cudaSetDevice(prev);
+  }
+};
+
+bool aligned(const void *p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+constexpr float kDefaultCoef[3] = {3.4445f, -4.7750f, 2.0315f};
+constexpr int kDefaultSteps = 5;
+
+// Whether the entries of every X, A and B stay below kMaxEntry: they are bounded by the spectral norms, and those by the
+// polynomials' largest values over the singular values that can occur (at most 1 after the division by the norm).
+bool bounded(const float (*coef)[3], int steps) {
+  double top = 1.001;
+  for (int i = 0; i < steps; ++i) {
+    const double a = coef[i][0], b = coef[i][1], c = coef[i][2];
+    if (!(isfinite(a) && isfinite(b) && isfinite(c))) return false;
+    double next = 0.0, side = 0.0;
+    constexpr int kPoints = 4096;
+    for (int j = 0; j <= kPoints; ++j) {
+      const double s = top * j / kPoints, q = s * s, r = q * (b + c * q);
+      next = std::max(next, fabs(s * (a + r)));
+      side = std::max(side, fabs(r));
+    }
+    if (!(top * top < kMaxEntry && side < kMaxEntry && next < kMaxEntry)) return false;
+    top = next * 1.001;  // between the points, and rounding
+  }
+  return true;
+}
+
+struct Layout {
+  std::vector<Group> groups;
+  std::vector<long long> offset;
+  std::vector<float> scale;
+  int chunks = 0, rblks = 0;
+  long long n_done = 0, most_tiles = 0;
+  size_t groups_at, maps_at, offset_at, scale_at, done_at, sumsq_at, error_at, tables, bytes;
+};
+
+dasgd_status layout(const dasgd_ortho_config *c, const char *who, int cg, Layout &o) {
+  const std::string at = std::string(who) + ": ";
+  // matrices of one shape form a group, in the order of their first appearance
+  std::vector<std::vector<int>> members;
+  for (int i = 0; i < c->n_matrices; ++i) {
+    const dasgd_matrix &m = c->matrices[i];
+    size_t g = 0;
+    while (g < o.groups.size() && (o.groups[g].rows != m.rows || o.groups[g].cols != m.cols)) ++g;
+    if (g == o.groups.size()) {
+      o.groups.emplace_back();
+      Group &n = o.groups.back();
+      memset(&n, 0, sizeof n);
+      n.rows = m.rows, n.cols = m.cols;
+      members.emplace_back();
+    }
+    members[g].push_back(i);
+  }
+  const int tile = 128 * cg;
+  long long chunks = 0, rblks = 0, tiles_all = 0, z0 = 0;
+  size_t big = 0;
+  auto take = [&](size_t n) {
+    const size_t x = big;
+    big += (n + 255) / 256 * 256;
+    return x;
+  };
+  for (size_t i = 0; i < o.groups.size(); ++i) {
+    Group &g = o.groups[i];
+    g.flip = g.rows > g.cols;
+    g.n = std::min(g.rows, g.cols), g.w = std::max(g.rows, g.cols);
+    g.matrices = (int)members[i].size();
+    const long long batch = (long long)g.matrices * c->K;
+    g.tn = (g.n + tile - 1) / tile, g.tw = (g.w + tile - 1) / tile;
+    const long long tg = (long long)g.tn * (g.tn + 1) / 2, tu = (long long)g.tn * g.tw;
+    g.ldx = (g.cols + 63) / 64 * 64, g.lda = (g.n + 63) / 64 * 64;
+    const long long numel = (long long)g.rows * g.cols;
+    const long long pieces = (numel + kChunk - 1) / kChunk;
+    g.rblk = std::max(1, kChunk / g.ldx);
+    g.rblks = (g.rows + g.rblk - 1) / g.rblk;
+    // a matrix's finished epilogue warps are counted in 32 bits, its tiles and pieces in int
+    if (tu >= (1 << 24) || pieces >= (1 << 30) || batch >= (1 << 30) || chunks + pieces * batch >= (1LL << 31) || rblks + g.rblks * batch >= (1LL << 31) ||
+        (long long)kMaxSteps * (2 * tg + tu) * cg * kEpiWarps >= (1LL << 31))
+      return unsupported(at + "too many or too large matrices for one call");
+    g.tg = (int)tg, g.tu = (int)tu, g.batch = (int)batch;
+    g.chunks = (int)pieces, g.chunk0 = (int)chunks, g.rblk0 = (int)rblks;
+    g.z0 = (int)z0, g.m0 = (int)o.offset.size();
+    chunks += pieces * batch, rblks += g.rblks * batch, z0 += batch;
+    tiles_all += tu * batch * 3;
+    o.most_tiles += std::max(tg, tu) * batch;
+    g.even = g.cols % 8 == 0 ? 2 : 1;
+    for (int m : members[i]) {
+      o.offset.push_back(c->matrices[m].offset), o.scale.push_back(c->matrices[m].scale);
+      if (c->matrices[m].offset % 8) g.even = 0;
+    }
+  }
+  if (tiles_all * kMaxSteps >= (1LL << 31) || z0 >= (1LL << 30)) return unsupported(at + "too many or too large matrices for one call");
+  o.chunks = (int)chunks, o.rblks = (int)rblks, o.n_done = z0;
+  o.groups_at = take(o.groups.size() * sizeof(Group));
+  o.maps_at = take(o.groups.size() * MAPS * sizeof(CUtensorMap));
+  o.offset_at = take(o.offset.size() * 8), o.scale_at = take(o.scale.size() * 4);
+  o.error_at = take(4);
+  o.tables = big;
+  o.done_at = take((size_t)z0 * 4), o.sumsq_at = take((size_t)chunks * 8);
+  const bool split = c->dtype == DASGD_F32;
+  for (Group &g : o.groups) {
+    const size_t x = (size_t)g.batch * g.rows * g.ldx * 2, a = (size_t)g.batch * g.n * g.lda * 2, d = (size_t)g.batch * g.lda * 4;
+    auto ptr = [&](size_t n) { return reinterpret_cast<__half *>(take(n)); };  // offsets for now
+    for (int b = 0; b < 2; ++b)
+      for (int part = 0; part < 2; ++part) g.x[b][part] = ptr(x);
+    for (int part = 0; part < 2; ++part) {
+      g.a[part] = part <= (int)split ? ptr(a) : g.a[0];
+      g.b[part] = part <= (int)split ? ptr(a) : g.b[0];
+    }
+    g.da = reinterpret_cast<float *>(take(d)), g.db = reinterpret_cast<float *>(take(d));
+  }
+  o.bytes = big;
+  return DASGD_OK;
+}
+
+dasgd_status check(const dasgd_ortho_config *c, const char *who) {
+  const std::string at = std::string(who) + ": ";
+  if (!c) return bad(at + "cfg is NULL");
+  if (c->K < 1 || c->K > 65535) return bad(at + "K must be in [1, 65535]");
+  if (c->dtype != DASGD_F32 && c->dtype != DASGD_BF16_MASTER_F32) return bad(at + "unknown dtype");
+  if (c->n_matrices < 1 || !c->matrices) return bad(at + "needs at least one matrix");
+  if (c->steps < 0 || c->steps > kMaxSteps) return bad(at + "steps must be in [1, 16] (0: the default)");
+  if (c->steps == 0 && c->coefficients) return bad(at + "coefficients need steps");
+  if (!(c->momentum >= 0.0f && isfinite(c->momentum))) return bad(at + "momentum must be >= 0");
+  if (c->nesterov && c->momentum == 0.0f) return bad(at + "nesterov needs momentum > 0");
+  if (!(c->eps >= 0.0f && isfinite(c->eps))) return bad(at + "eps must be >= 0");
+  if (c->tile != 0 && c->tile != 128 && c->tile != 256) return bad(at + "tile must be 0, 128 or 256");
+  if (c->device < 0) return bad(at + "device must be >= 0");
+  std::vector<std::pair<int64_t, int64_t>> spans;
+  for (int i = 0; i < c->n_matrices; ++i) {
+    const dasgd_matrix &m = c->matrices[i];
+    if (m.rows < 1 || m.cols < 1 || m.rows > (1 << 20) || m.cols > (1 << 20))
+      return bad(at + "rows and cols must be in [1, 2^20]");
+    if (m.offset < 0 || m.offset > c->ld || (int64_t)m.rows * m.cols > c->ld - m.offset)
+      return bad(at + "a matrix must lie inside a row: offset >= 0, offset + rows*cols <= ld");
+    if (!isfinite(m.scale)) return bad(at + "scale must be finite");
+    spans.emplace_back(m.offset, m.offset + (int64_t)m.rows * m.cols);
+  }
+  std::sort(spans.begin(), spans.end());
+  for (size_t i = 1; i < spans.size(); ++i)
+    if (spans[i].first < spans[i - 1].second) return bad(at + "matrices must not overlap");
+  return DASGD_OK;
+}
+
+void coefficients(const dasgd_ortho_config *c, int &steps, float (*coef)[3]) {
+  steps = c->steps ? c->steps : kDefaultSteps;
+  for (int i = 0; i < steps; ++i)
+    for (int j = 0; j < 3; ++j) coef[i][j] = c->coefficients ? c->coefficients[3 * i + j] : kDefaultCoef[j];
+}
+
+int choose_tile(const dasgd_ortho_config *c) { return c->tile ? c->tile / 128 : 1; }
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+  void *f = nullptr;
+  cudaDriverEntryPointQueryResult q;
+  if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+      q != cudaDriverEntryPointSuccess)
+    return nullptr;
+  return reinterpret_cast<EncodeTiled>(f);
+}
+
+bool encode(EncodeTiled enc, CUtensorMap *map, void *base, int rows, int cols, int ld, int batch) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
+  const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
+  const cuuint32_t box[3] = {kBox, kBox, 1}, step[3] = {1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename F>
+dasgd_status with_kernel(int cg, int dtype, F f) {
+  if (dtype == DASGD_F32) return cg == 1 ? f(k_ortho_steps<1, true, float>, (float *)nullptr) : f(k_ortho_steps<2, true, float>, (float *)nullptr);
+  return cg == 1 ? f(k_ortho_steps<1, false, __nv_bfloat16>, (__nv_bfloat16 *)nullptr)
+                 : f(k_ortho_steps<2, false, __nv_bfloat16>, (__nv_bfloat16 *)nullptr);
+}
+
+void launch_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&attr)[2], int cg, int grid, cudaStream_t s) {
+  lc = cudaLaunchConfig_t{};
+  lc.gridDim = dim3(grid), lc.blockDim = dim3(kThreads), lc.dynamicSmemBytes = kSmemBytes, lc.stream = s;
+  attr[0].id = cudaLaunchAttributeCooperative, attr[0].val.cooperative = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cg, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+  lc.attrs = attr, lc.numAttrs = cg == 1 ? 1 : 2;
+}
+
+template <typename T>
+dasgd_status run(const dasgd_ortho *op, const T *g, float *m, T *out, cudaStream_t s) {
+  const int vec = op->plan.ld % 8 == 0 && aligned(g, 16) && aligned(m, 16), vec_out = op->plan.ld % 8 == 0 && aligned(out, 16);
+  k_ortho_momentum<T><<<op->chunks, kPrepThreads, 0, s>>>(op->plan, g, m, vec);
+  k_ortho_scale<T><<<op->rblks, kPrepThreads, 0, s>>>(op->plan, g, m, vec);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return cuda_fail(e, "ortho_step");
+  return with_kernel(op->cg, op->dtype, [&](auto kernel, auto *type) -> dasgd_status {
+    using Out = std::remove_pointer_t<decltype(type)>;
+    if constexpr (std::is_same_v<Out, T>) {
+      cudaLaunchConfig_t lc;
+      cudaLaunchAttribute attr[2];
+      launch_config(lc, attr, op->cg, op->grid, s);
+      const cudaError_t err = cudaLaunchKernelEx(&lc, kernel, op->plan, out, vec_out);
+      return err == cudaSuccess ? DASGD_OK : cuda_fail(err, "ortho_step");
+    }
+    return DASGD_OK;
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+dasgd_status dasgd_ortho_workspace(const dasgd_ortho_config *cfg, int64_t *bytes) {
+  dasgd_status st = check(cfg, "ortho_workspace");
+  if (st != DASGD_OK) return st;
+  if (!bytes) return bad("ortho_workspace: bytes is NULL");
+  try {
+    Layout l;
+    st = layout(cfg, "ortho_workspace", choose_tile(cfg), l);
+    if (st == DASGD_OK) *bytes = (int64_t)l.bytes;
+    return st;
+  } catch (const std::bad_alloc &) {
+    return unsupported("ortho_workspace: out of host memory");
+  }
+}
+
+dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, void *stream) try {
+  if (!out) return bad("ortho_init: out is NULL");
+  *out = nullptr;
+  dasgd_status st = check(cfg, "ortho_init");
+  if (st != DASGD_OK) return st;
+  const dasgd_ortho_config &c = *cfg;
+  Plan p{};
+  coefficients(cfg, p.steps, p.coef);
+  if (!bounded(p.coef, p.steps))
+    return unsupported("ortho_init: these coefficients let the iterates grow past the range of the fp16 operands");
+  const int cg = choose_tile(cfg);
+  Layout l;
+  st = layout(cfg, "ortho_init", cg, l);
+  if (st != DASGD_OK) return st;
+  if (!c.workspace || !aligned(c.workspace, 256) || c.workspace_bytes < (int64_t)l.bytes)
+    return bad("ortho_init: needs a 256-byte aligned workspace of " + std::to_string(l.bytes) + " bytes");
+  OnDevice dev(c.device);
+  if (dev.e != cudaSuccess) return cuda_fail(dev.e, "ortho_init");
+  cudaPointerAttributes pa;
+  cudaError_t e = cudaPointerGetAttributes(&pa, c.workspace);
+  if (e != cudaSuccess || pa.type != cudaMemoryTypeDevice || pa.device != c.device) {
+    cudaGetLastError();
+    return bad("ortho_init: the workspace must be device memory of cfg.device");
+  }
+  EncodeTiled enc = encoder();
+  if (!enc) return dasgd_internal_fail(nullptr, DASGD_ERR_CUDA, "ortho_init: the driver has no cuTensorMapEncodeTiled");
+
+  char *ws = static_cast<char *>(c.workspace);
+  auto at = [&](auto *&ptr) { ptr = reinterpret_cast<std::remove_reference_t<decltype(ptr)>>(ws + reinterpret_cast<size_t>(ptr)); };
+  std::vector<char> host(l.tables, 0);
+  CUtensorMap *maps = reinterpret_cast<CUtensorMap *>(host.data() + l.maps_at);
+  for (size_t i = 0; i < l.groups.size(); ++i) {
+    Group &g = l.groups[i];
+    for (int part = 0; part < 2; ++part) {
+      at(g.x[0][part]), at(g.x[1][part]), at(g.a[part]), at(g.b[part]);
+      CUtensorMap *mi = maps + i * MAPS;
+      for (int b = 0; b < 2; ++b)
+        if (!encode(enc, mi + MAP_X + 2 * b + part, g.x[b][part], g.rows, g.cols, g.ldx, g.batch))
+          return dasgd_internal_fail(nullptr, DASGD_ERR_CUDA, "ortho_init: cuTensorMapEncodeTiled failed");
+      if (!encode(enc, mi + MAP_A + part, g.a[part], g.n, g.n, g.lda, g.batch) || !encode(enc, mi + MAP_B + part, g.b[part], g.n, g.n, g.lda, g.batch))
+        return dasgd_internal_fail(nullptr, DASGD_ERR_CUDA, "ortho_init: cuTensorMapEncodeTiled failed");
+    }
+    at(g.da), at(g.db);
+  }
+  memcpy(host.data() + l.groups_at, l.groups.data(), l.groups.size() * sizeof(Group));
+  memcpy(host.data() + l.offset_at, l.offset.data(), l.offset.size() * 8);
+  memcpy(host.data() + l.scale_at, l.scale.data(), l.scale.size() * 4);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if ((e = cudaMemcpyAsync(ws, host.data(), l.tables, cudaMemcpyHostToDevice, s)) != cudaSuccess || (e = cudaStreamSynchronize(s)) != cudaSuccess)
+    return cuda_fail(e, "ortho_init");
+
+  p.groups = reinterpret_cast<const Group *>(ws + l.groups_at), p.maps = reinterpret_cast<const CUtensorMap *>(ws + l.maps_at);
+  p.offset = reinterpret_cast<const long long *>(ws + l.offset_at), p.scale = reinterpret_cast<const float *>(ws + l.scale_at);
+  p.done = reinterpret_cast<unsigned *>(ws + l.done_at), p.sumsq = reinterpret_cast<double *>(ws + l.sumsq_at);
+  p.error = reinterpret_cast<int *>(ws + l.error_at);
+  p.n_groups = (int)l.groups.size(), p.K = c.K, p.n_done = (int)l.n_done, p.ld = c.ld;
+  p.mu = c.momentum, p.eps = c.eps, p.nesterov = c.nesterov != 0;
+  p.timeout_ns = (c.timeout_ms ? c.timeout_ms : 10000u) * 1000000ull;
+
+  int sms = 0, clusters = 0;
+  st = with_kernel(cg, c.dtype, [&](auto kernel, auto *) -> dasgd_status {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c.device);
+    if (e == cudaSuccess && cg == 2) {
+      cudaLaunchConfig_t lc;
+      cudaLaunchAttribute attr[2];
+      launch_config(lc, attr, cg, sms / 2 * 2, s);
+      e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
+    }
+    return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "ortho_init");
+  });
+  if (st != DASGD_OK) return st;
+  const long long room = cg == 2 ? std::min(clusters, sms / 2) : sms;
+  if (room < 1) return unsupported("ortho_init: the kernel does not fit this GPU");
+  dasgd_ortho *op = new dasgd_ortho;
+  op->plan = p, op->device = c.device, op->dtype = c.dtype, op->cg = cg, op->chunks = l.chunks, op->rblks = l.rblks;
+  op->has_momentum = c.momentum != 0.0f;
+  op->grid = (int)std::min(l.most_tiles, room) * cg;
+  *out = op;
+  return DASGD_OK;
+} catch (const std::bad_alloc &) {
+  return unsupported("ortho_init: out of host memory");
+}
+
+dasgd_status dasgd_ortho_step(dasgd_ortho *op, const void *g, float *m, void *out, void *stream) {
+  if (!op) return bad("ortho_step: NULL operator");
+  if (!g || !out) return bad("ortho_step: g and out must not be NULL");
+  if (op->has_momentum != (m != nullptr)) return bad("ortho_step: m must be given exactly when momentum != 0");
+  const size_t el = op->dtype == DASGD_F32 ? 4 : 2;
+  if (!aligned(g, el) || !aligned(out, el) || !aligned(m, 4)) return bad("ortho_step: buffers must be aligned to their elements");
+  OnDevice dev(op->device);
+  if (dev.e != cudaSuccess) return cuda_fail(dev.e, "ortho_step");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (op->dtype == DASGD_F32) return run(op, static_cast<const float *>(g), m, static_cast<float *>(out), s);
+  return run(op, static_cast<const __nv_bfloat16 *>(g), m, static_cast<__nv_bfloat16 *>(out), s);
+}
+
+dasgd_status dasgd_ortho_sync(dasgd_ortho *op, void *stream) {
+  if (!op) return bad("ortho_sync: NULL operator");
+  OnDevice dev(op->device);
+  if (dev.e != cudaSuccess) return cuda_fail(dev.e, "ortho_sync");
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  int flag = 0;
+  cudaError_t e = cudaMemcpyAsync(&flag, op->plan.error, sizeof flag, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e == cudaSuccess && flag) {
+    e = cudaMemsetAsync(op->plan.error, 0, sizeof flag, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  }
+  if (e != cudaSuccess) return cuda_fail(e, "ortho_sync");
+  if (flag) return dasgd_internal_fail(nullptr, DASGD_ERR_TIMEOUT, "ortho_sync: a wait on the GPU ran out of time; the directions of that step are not valid");
+  return DASGD_OK;
+}
+
+dasgd_status dasgd_ortho_destroy(dasgd_ortho *op) {
+  if (!op) return bad("ortho_destroy: NULL operator");
+  delete op;
+  return DASGD_OK;
+}
+
+}  // extern "C"

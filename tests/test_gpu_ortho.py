@@ -1,0 +1,271 @@
+"""Orthogonalised directions against the formula in 64 bits.
+
+Tolerances, relative in the 2-norm of a matrix, written down before the first run.  A step rounds five operands (the iterate
+for the Gram product, A, B, the iterate for the update, the new iterate); five steps make 25 roundings whose errors are at
+most added up: products keep the norm of what is near orthogonal, and the error of the weak directions grows as they do.
+  bfloat16: fp16 operands, 2^-12 root mean square each, and the output's own rounding, below 2^-9 root mean square:
+            25 * 2^-12 + 2^-9 = 8.1e-3.
+  float32:  pairs of fp16, 2^-22 each, and sums of w/16 float32 partial products per entry whose roundings (2^-24) have
+            random signs: 25 * (2^-22 + sqrt(w/16) * 2^-24).
+The momentum array is two float32 operations from exact: 2^-23 * (|mu m| + |g|) for every element.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+COEF = (3.4445, -4.7750, 2.0315)
+F32, BF16 = 0, 1
+
+
+def tolerance(dtype, w, steps=5):
+    return steps * 5 * 2.0 ** -12 + 2.0 ** -9 if dtype == BF16 else steps * 5 * (2.0 ** -22 + math.sqrt(w / 16) * 2.0 ** -24)
+
+
+def newton_schulz(u, steps, coef, eps=1e-7):
+    x = u.double()
+    x = x / (torch.linalg.matrix_norm(x) + eps)
+    tall = x.shape[0] > x.shape[1]
+    x = x.T if tall else x
+    for i in range(steps):
+        a, b, c = coef[i] if isinstance(coef[0], tuple) else coef
+        A = x @ x.T
+        x = a * x + (b * A + c * A @ A) @ x
+    return x.T if tall else x
+
+
+def sample(gen, r, c, kind):
+    x = torch.randn(r, c, generator=gen, device="cuda")
+    if kind == "flat":
+        return x
+    n = min(r, c)
+    q = max(1, n // 16)
+    low = torch.randn(r, q, generator=gen, device="cuda") @ torch.randn(q, c, generator=gen, device="cuda") / math.sqrt(q)
+    return low + {"noisy": 0.1, "decaying": 0.01}[kind] * x
+
+
+def check(shapes, K=1, dtype=F32, gap=0, mu=0.95, nesterov=True, steps=5, coef=None, tile=0, kind="noisy", seed=0, inplace=False, misalign=0, scales=None):
+    from paper_2006_00441_b200 import binding as B
+    gen = torch.Generator("cuda").manual_seed(seed)
+    places, at = [], gap
+    for i, (r, c) in enumerate(shapes):
+        places.append((at, r, c, scales[i] if scales else 1.0))
+        at += r * c + gap
+    ld = at
+    gd = torch.bfloat16 if dtype == BF16 else torch.float32
+
+    def array(dt):
+        return torch.zeros(K * ld + misalign, dtype=dt, device="cuda")[misalign:].view(K, ld)
+
+    g, m, out = array(gd), array(torch.float32), array(gd)
+    g.fill_(7.0), m.fill_(5.0), out.fill_(3.0)      # what lies between the matrices must survive
+    for o, r, c, _ in places:
+        for k in range(K):
+            g[k, o:o + r * c] = (1e-3 * sample(gen, r, c, kind)).reshape(-1).to(gd)
+            m[k, o:o + r * c] = (5e-3 * sample(gen, r, c, kind)).reshape(-1)
+    g0, m0 = g.clone(), m.clone()
+    op = B.Ortho(K, ld, places, dtype=dtype, momentum=mu, nesterov=nesterov, steps=steps, coefficients=coef, tile=tile)
+    got = op.step(g, m if mu else None, out=None if inplace else out)
+    op.sync()
+    covered = torch.zeros(ld, dtype=torch.bool, device="cuda")
+    worst = 0.0
+    for o, r, c, s in places:
+        covered[o:o + r * c] = True
+        for k in range(K):
+            here = slice(o, o + r * c)
+            u = g0[k, here].double()
+            if mu:
+                m1 = mu * m0[k, here].double() + u
+                assert bool(((m[k, here].double() - m1).abs() <= 2.0 ** -23 * ((mu * m0[k, here]).double().abs() + u.abs()) + 1e-7 * m1.abs()).all())
+                u = u + mu * m1 if nesterov else m1
+            want = s * newton_schulz(u.view(r, c), steps, coef or COEF)
+            err = float(torch.linalg.matrix_norm(got[k, here].view(r, c).double() - want) / torch.linalg.matrix_norm(want))
+            worst = max(worst, err / tolerance(dtype, max(r, c), steps))
+            assert err <= tolerance(dtype, max(r, c), steps), (r, c, k, err)
+    if not inplace:
+        assert torch.equal(g, g0) and bool((out[:, ~covered] == 3.0).all())
+    else:
+        assert torch.equal(g[:, ~covered], g0[:, ~covered])
+    assert torch.equal(m[:, ~covered], m0[:, ~covered])
+    if not mu:
+        assert torch.equal(m, m0)
+    op.close()
+    return worst
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tile", [128, 256])
+@pytest.mark.parametrize("r,c", [(1, 1), (1, 300), (300, 1), (8, 8), (63, 65), (64, 64), (127, 129), (128, 128), (129, 128), (256, 256), (257, 255),
+                                 (100, 1000), (1000, 100), (511, 640), (640, 511)])
+def test_one_matrix(r, c, tile, dtype):
+    check([(r, c)], dtype=dtype, tile=tile, seed=r + c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tile", [0, 128, 256])
+@pytest.mark.parametrize("K,shapes,gap", [(3, [(96, 200), (200, 96), (96, 200), (33, 7)], 5), (2, [(512, 512), (512, 512), (1024, 256), (256, 1024)], 8),
+                                          (5, [(130, 390)], 0)])
+def test_groups_of_matrices_in_replicas(K, shapes, gap, tile, dtype):
+    check(shapes, K=K, dtype=dtype, gap=gap, tile=tile, scales=[0.5 + i for i in range(len(shapes))])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["flat", "noisy", "decaying"])
+@pytest.mark.parametrize("r,c", [(1024, 1024), (768, 2304), (2304, 768)])
+def test_spectra(r, c, kind, dtype):
+    check([(r, c)], dtype=dtype, kind=kind)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_large(dtype):
+    check([(4096, 4096)], dtype=dtype)
+
+
+@pytest.mark.parametrize("mu,nesterov", [(0.0, False), (0.9, False), (0.95, True)])
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_momentum_forms_and_in_place(mu, nesterov, inplace, dtype):
+    check([(200, 136), (72, 264)], K=2, dtype=dtype, mu=mu, nesterov=nesterov, inplace=inplace, gap=3)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_arrays_that_are_not_16_byte_aligned(dtype):
+    check([(128, 256), (64, 64)], K=2, dtype=dtype, misalign=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("coef", [(1.5, -0.5, 0.0), (2.0, -1.5, 0.5), ((4.0, -6.0, 2.4), (3.4445, -4.775, 2.0315), (1.875, -1.25, 0.375))])
+def test_other_polynomials(coef, dtype):
+    check([(160, 320)], dtype=dtype, coef=coef, steps=len(coef) if isinstance(coef[0], tuple) else 3, kind="flat")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_zero_matrix_gives_zero_and_nan_stays_in_its_matrix(dtype):
+    from paper_2006_00441_b200 import binding as B
+    K, n = 3, 130
+    gd = torch.bfloat16 if dtype == BF16 else torch.float32
+    g = torch.randn(K, 2 * n * n, device="cuda").to(gd)
+    g[0, :n * n] = 0
+    g[1, 17] = float("nan")
+    g[2, n * n + 5] = float("inf")
+    op = B.Ortho(K, 2 * n * n, [(0, n, n), (n * n, n, n)], dtype=dtype, momentum=0.0)
+    out = op.step(g, out=torch.empty_like(g))
+    op.sync()
+    assert bool((out[0, :n * n] == 0).all())
+    assert bool(out[1, :n * n].isnan().any()) and bool(out[2, n * n:].isnan().any())
+    assert bool(out[0, n * n:].isfinite().all()) and bool(out[1, n * n:].isfinite().all()) and bool(out[2, :n * n].isfinite().all())
+    ok = newton_schulz(g[2, :n * n].view(n, n), 5, COEF)
+    assert float(torch.linalg.matrix_norm(out[2, :n * n].view(n, n).double() - ok) / torch.linalg.matrix_norm(ok)) <= tolerance(dtype, n)
+
+
+@pytest.mark.parametrize("size", [1e-18, 1e-6, 1e6, 1e15])
+def test_the_size_of_the_gradient_does_not_matter(size):
+    from paper_2006_00441_b200 import binding as B
+    g = torch.randn(1, 100 * 60, device="cuda") * size
+    op = B.Ortho(1, 6000, [(0, 100, 60)], momentum=0.0, eps=0.0)
+    out = op.step(g, out=torch.empty_like(g))
+    want = newton_schulz(g.view(100, 60), 5, COEF, 0.0)
+    assert float(torch.linalg.matrix_norm(out.view(100, 60).double() - want) / torch.linalg.matrix_norm(want)) <= tolerance(F32, 100)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_equal_inputs_give_equal_bits(dtype):
+    from paper_2006_00441_b200 import binding as B
+    gd = torch.bfloat16 if dtype == BF16 else torch.float32
+    g = torch.randn(2, 600 * 700, device="cuda").to(gd)
+    outs = []
+    for tile in (128, 128, 256, 256):
+        op = B.Ortho(2, 600 * 700, [(0, 600, 700)], dtype=dtype, momentum=0.0, tile=tile)
+        outs.append([op.step(g, out=torch.empty_like(g)) for _ in range(3)])
+        op.sync()
+    assert all(torch.equal(o, outs[0][0]) for o in outs[0] + outs[1]) and all(torch.equal(o, outs[2][0]) for o in outs[2] + outs[3])
+
+
+def test_calls_on_different_streams_share_the_workspace_safely():
+    from paper_2006_00441_b200 import binding as B
+    op = B.Ortho(2, 512 * 512, [(0, 512, 512)], momentum=0.0)
+    jobs = [(torch.randn(2, 512 * 512, device="cuda"), torch.empty(2, 512 * 512, device="cuda"), torch.cuda.Stream()) for _ in range(6)]
+    torch.cuda.synchronize()
+    for g, out, s in jobs:
+        with torch.cuda.stream(s):
+            op.step(g, out=out)
+    torch.cuda.synchronize()
+    for g, out, _ in jobs:
+        for k in range(2):
+            want = newton_schulz(g[k].view(512, 512), 5, COEF)
+            assert float(torch.linalg.matrix_norm(out[k].view(512, 512).double() - want) / torch.linalg.matrix_norm(want)) <= tolerance(F32, 512)
+
+
+def test_two_operators_on_two_streams_at_once():
+    """Both launches want every SM and wait inside for their own CTAs: neither may start by halves."""
+    from paper_2006_00441_b200 import binding as B
+    n = 1024
+    ops = [B.Ortho(4, n * n, [(0, n, n)], momentum=0.0, tile=t) for t in (128, 256)]
+    g = torch.randn(4, n * n, device="cuda")
+    outs, streams = [torch.empty_like(g) for _ in ops], [torch.cuda.Stream() for _ in ops]
+    torch.cuda.synchronize()
+    for _ in range(8):
+        for op, out, s in zip(ops, outs, streams):
+            with torch.cuda.stream(s):
+                op.step(g, out=out)
+    for op in ops:
+        op.sync()
+    want = newton_schulz(g[3].view(n, n), 5, COEF)
+    for out in outs:
+        assert float(torch.linalg.matrix_norm(out[3].view(n, n).double() - want) / torch.linalg.matrix_norm(want)) <= tolerance(F32, n)
+
+
+def test_the_direction_in_the_gradient_array_is_what_the_engine_subtracts():
+    from paper_2006_00441_b200 import binding as B
+    K, r, c, tail = 4, 96, 160, 40
+    P = r * c + tail
+    for dtype in (F32, BF16):
+        eng = B.DaSGD(K, P, tau=2, d=1, xi=0.25, dtype=dtype)
+        w0 = torch.randn(P)
+        eng.set_state(w0)
+        g = torch.randn(K, P, device="cuda").to(eng.gdtype)
+        raw = g.clone()
+        m = torch.zeros(K, P, device="cuda")
+        op = B.Ortho(K, P, [(0, r, c)], dtype=dtype)
+        op.step(g, m)
+        eng.step(g, 0.02)
+        eng.sync()
+        want = w0.cuda() - 0.02 * g.float()
+        assert torch.equal(g[:, r * c:], raw[:, r * c:])
+        assert bool(((eng.w[:, :P] - want).abs() <= 1e-6 * (1 + want.abs())).all())
+        eng.close()
+
+
+def test_a_wait_that_runs_out_of_time_is_reported():
+    """One large matrix on a 1 ms limit: CTAs without a tile of the running product wait for it longer than that, give up in
+    order and say so; the operator is usable afterwards."""
+    from paper_2006_00441_b200 import binding as B
+    n = 16384
+    g = torch.randn(1, n * n, device="cuda")
+    op = B.Ortho(1, n * n, [(0, n, n)], momentum=0.0, steps=1, timeout_ms=1)
+    op.step(g, out=torch.empty_like(g))
+    with pytest.raises(B.DasgdError) as e:
+        op.sync()
+    assert e.value.status == B.DASGD_ERR_TIMEOUT
+    op.close()
+    small = B.Ortho(1, n * n, [(0, 256, 256)], momentum=0.0)
+    out = small.step(g, out=torch.empty_like(g))
+    small.sync()
+    want = newton_schulz(g[0, :65536].view(256, 256), 5, COEF)
+    assert float(torch.linalg.matrix_norm(out[0, :65536].view(256, 256).double() - want) / torch.linalg.matrix_norm(want)) <= tolerance(F32, 256)
+
+
+def test_wrapper_refuses_what_it_cannot_take():
+    from paper_2006_00441_b200 import binding as B
+    op = B.Ortho(2, 64, [(0, 8, 8)])
+    g, m = torch.zeros(2, 64, device="cuda"), torch.zeros(2, 64, device="cuda")
+    for bad in (lambda: op.step(g), lambda: op.step(g.bfloat16(), m), lambda: op.step(g[:1], m), lambda: op.step(g, m[:, :63]), lambda: op.step(g.cpu(), m),
+                lambda: op.step(g, m, out=g.half())):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(ValueError):
+        B.Ortho(2, 64, [(0, 8, 8)], steps=3, coefficients=[(1.5, -0.5, 0.0)] * 2)
+    with pytest.raises(B.DasgdError) as e:
+        B.Ortho(2, 64, [(0, 8, 8)], coefficients=(30.0, 0.0, 0.0))
+    assert e.value.status == B.DASGD_ERR_UNSUPPORTED

@@ -58,11 +58,63 @@ def test_embedding_workspace_serves_fewer_tokens(K, V, D):
     assert sizes == sorted(sizes)
 
 
+def _ortho(matrices=((0, 8, 8),), **kw):
+    c = B.dasgd_ortho_config()
+    c.K, c.n_matrices, c.dtype, c.ld, c.momentum, c.nesterov, c.eps = 2, len(matrices), 0, 200, 0.9, 1, 1e-7
+    c.matrices = (B.dasgd_matrix * max(1, len(matrices)))(*(B.dasgd_matrix(*m, *((1.0,) if len(m) == 3 else ())) for m in matrices))
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return c
+
+
+@pytest.mark.parametrize("bad,frag", [
+    (dict(K=0), "K must"), (dict(dtype=5), "dtype"), (dict(n_matrices=0), "at least one"), (dict(steps=17), "steps must"), (dict(steps=-1), "steps must"),
+    (dict(momentum=-0.1), "momentum"), (dict(momentum=float("nan")), "momentum"), (dict(momentum=0.0), "nesterov"), (dict(eps=-1.0), "eps"),
+    (dict(tile=64), "tile"), (dict(device=-1), "device"), (dict(ld=63), "inside a row"), (dict(matrices=((-1, 8, 8),)), "inside a row"),
+    (dict(matrices=((0, 0, 8),)), "rows and cols"), (dict(matrices=((0, 8, 1 << 21),)), "rows and cols"), (dict(matrices=((0, 8, 8), (63, 8, 8))), "overlap"),
+    (dict(matrices=((0, 8, 8, float("inf")),)), "scale"),
+])
+def test_ortho_configuration_is_checked(bad, frag):
+    c = _ortho(**bad)
+    for call in (lambda: B.dasgd_ortho_workspace(c), lambda: B.dasgd_ortho_init(c, None)):
+        with pytest.raises(B.DasgdError) as e:
+            call()
+        assert e.value.status == B.DASGD_ERR_INVALID_ARG and frag in str(e.value)
+
+
+def test_ortho_refuses_polynomials_that_leave_the_range_of_its_operands():
+    for coef, steps in (([30.0, 0.0, 0.0], 1), ([3.0, 3.0, 3.0] * 4, 4), ([float("nan"), 0.0, 0.0], 1)):
+        c = _ortho(steps=steps)
+        c.coefficients = (ctypes.c_float * len(coef))(*coef)
+        with pytest.raises(B.DasgdError) as e:
+            B.dasgd_ortho_init(c, None)
+        assert e.value.status == B.DASGD_ERR_UNSUPPORTED
+
+
+def test_ortho_null_arguments_and_small_workspaces():
+    c = _ortho()
+    n = B.dasgd_ortho_workspace(c)
+    assert n > 0
+    for ws, size in ((None, n), (0x1000, n - 1), (0x1010, n)):
+        c.workspace, c.workspace_bytes = ws, size
+        with pytest.raises(B.DasgdError) as e:
+            B.dasgd_ortho_init(c, None)
+        assert "workspace" in str(e.value)
+    for call in (B._L.dasgd_ortho_workspace(None, None), B._L.dasgd_ortho_init(None, ctypes.byref(c), None), B._L.dasgd_ortho_step(None, None, None, None, None),
+                 B._L.dasgd_ortho_sync(None, None), B._L.dasgd_ortho_destroy(None)):
+        assert call == B.DASGD_ERR_INVALID_ARG
+
+
+def test_ortho_workspace_holds_float32_operands_in_pairs():
+    lo, hi = (B.dasgd_ortho_workspace(_ortho(((0, 100, 1000),), dtype=d, ld=100000)) for d in (1, 0))
+    assert hi > lo > 2 * 100000 * 8
+
+
 def test_embedding_config_layout_matches_the_binding(tmp_path):
     import os
     import subprocess
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    for name, mirror in [("dasgd_embed_config", B.dasgd_embed_config)]:
+    for name, mirror in [("dasgd_embed_config", B.dasgd_embed_config), ("dasgd_matrix", B.dasgd_matrix), ("dasgd_ortho_config", B.dasgd_ortho_config)]:
         fields = [f[0] for f in mirror._fields_]
         src = tmp_path / f"{name}.c"
         src.write_text('#include "dasgd.h"\n#include <stddef.h>\n#include <stdio.h>\nint main(void) {\n'
