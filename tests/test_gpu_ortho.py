@@ -238,18 +238,18 @@ def test_the_direction_in_the_gradient_array_is_what_the_engine_subtracts():
 
 
 def test_a_wait_that_runs_out_of_time_is_reported():
-    """One large matrix on a 1 ms limit: CTAs without a tile of the running product wait for it longer than that, give up in
-    order and say so; the operator is usable afterwards."""
+    """A long thin matrix on a 1 ms limit: its Gram product is a single tile, 2^20 long, that takes several milliseconds, and the
+    CTAs that are to update the matrix wait for it.  They give up in order and say so; a new operator works afterwards."""
     from paper_2006_00441_b200 import binding as B
-    n = 16384
-    g = torch.randn(1, n * n, device="cuda")
-    op = B.Ortho(1, n * n, [(0, n, n)], momentum=0.0, steps=1, timeout_ms=1)
+    r, c = 128, 1 << 20
+    g = torch.randn(1, r * c, device="cuda")
+    op = B.Ortho(1, r * c, [(0, r, c)], momentum=0.0, steps=1, timeout_ms=1)
     op.step(g, out=torch.empty_like(g))
     with pytest.raises(B.DasgdError) as e:
         op.sync()
     assert e.value.status == B.DASGD_ERR_TIMEOUT
     op.close()
-    small = B.Ortho(1, n * n, [(0, 256, 256)], momentum=0.0)
+    small = B.Ortho(1, r * c, [(0, 256, 256)], momentum=0.0)
     out = small.step(g, out=torch.empty_like(g))
     small.sync()
     want = newton_schulz(g[0, :65536].view(256, 256), 5, COEF)
