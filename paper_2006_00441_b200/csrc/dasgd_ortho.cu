@@ -48,12 +48,13 @@ constexpr double kMaxEntry = 15.0;                        // * kStore < 65504
 constexpr int kBox = 64;                                  // TMA box: 64 x 64 fp16, 8 KB, rows of 128 bytes
 constexpr int kBoxBytes = kBox * kBox * 2;
 constexpr int kSlotBytes = 4 * kBoxBytes;                 // 128 x 64 of either operand
-constexpr int kSlots = 6;
+constexpr int kSlots = 5;
 constexpr int kEpiWarps = 8, kThreads = 128 + kEpiWarps * 32;
-constexpr int kSmemBytes = kSlots * kSlotBytes + 1024;    // + slack to start on a 1024-byte boundary
+constexpr int kStageRows = 32, kStagePart = kStageRows * 128, kStage = 2 * kStagePart;  // an epilogue warp's 32 x 64 pairs
 
 enum { GRAM = 0, SQUARE = 1, UPDATE = 2 };
-enum { MAP_X = 0, MAP_A = 4, MAP_B = 6, MAPS = 8 };       // MAP_X + 2 * buffer + part; MAP_A + part; MAP_B + part
+enum { MAP_X = 0, MAP_A = 4, MAP_B = 6, MAP_EPI = 8, MAPS = 16 };  // MAP_X + 2 * buffer + part; MAP_A + part; MAP_B + part; + MAP_EPI: the
+                                                                   // same arrays in the epilogues' boxes of 32 rows
 
 struct Group {                                            // matrices of one shape, all replicas
   int rows, cols, n, w, flip;                             // n = the smaller side; flip: n is the columns
@@ -257,7 +258,7 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar, int rank) {
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   uint32_t ok;
   asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
       : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
@@ -319,19 +320,34 @@ __device__ __forceinline__ void tmem_free(uint32_t addr, int cols) {
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
 }
 
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
-  uint32_t r[32];
+__device__ __forceinline__ void tmem_load64(uint32_t addr, float (&v)[64]) {
+  uint32_t r[64];
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,"
-      "%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n tcgen05.wait::ld.sync.aligned;"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
-        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
-        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      "tcgen05.ld.sync.aligned.32x32b.x64.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,"
+      "%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,"
+      "%59,%60,%61,%62,%63"
+      "}, [%64];\n tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), 
+        "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), 
+        "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), 
+        "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), 
+        "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), 
+        "=r"(r[46]), "=r"(r[47]), "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), 
+        "=r"(r[55]), "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
       : "r"(addr) : "memory");
 #pragma unroll
-  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+  for (int i = 0; i < 64; ++i) v[i] = __uint_as_float(r[i]);
 }
+
+// a box of shared memory to a tensor; the box is cut at the tensor's edges
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+               ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 __device__ __forceinline__ void cluster_barrier() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -412,10 +428,14 @@ __device__ __forceinline__ bool outer(const Operand &o, int kb) {  // whether th
 }
 
 struct Shared {
-  uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2];
+  uint8_t slots[kSlots][kSlotBytes];
+  uint8_t stage[kEpiWarps][kStage];
+  float columns[kEpiWarps][64];          // what an epilogue warp needs of the other side's diagonal
+  uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2], in[kEpiWarps];
   uint32_t tmem;
   volatile int abort;
 };
+static_assert(sizeof(Shared) <= 227 * 1024, "shared memory of a CTA");
 
 // Waits give up after the plan's time limit, or once another wait of this CTA has: the error word is set, all roles leave
 // their loops, and the CTA ends in order.
@@ -432,19 +452,34 @@ struct Patience {
     atomicExch(error, 1);
     return true;
   }
+  // Both are called by whole warps and answer the same to every lane.
   __device__ bool bar(uint32_t b, uint32_t parity) {
     since = 0;
-    for (int i = 1; !mbar_try(b, parity); ++i)
-      if ((i & 63) == 0 && over()) return false;
+    for (int i = 1; !__all_sync(0xffffffffu, mbar_try(b, parity)); ++i)
+      if ((i & 63) == 0 && __any_sync(0xffffffffu, over())) return false;
     return true;
   }
   __device__ bool count(const unsigned *p, unsigned want) {  // want <= 2^31: counts never wrap
     since = 0;
-    for (int i = 1; load_acquire(p) < want; ++i)
-      if ((i & 63) == 0 && over()) return false;
+    for (int i = 1; !__all_sync(0xffffffffu, load_acquire(p) >= want); ++i)
+      if ((i & 63) == 0 && __any_sync(0xffffffffu, over())) return false;
     return true;
   }
 };
+
+// One lane of a converged warp.  Issuing under this predicate, with the loops around it run by the whole warp, keeps the
+// operands of loads and products in uniform registers; under `lane == 0` each one cost about a hundred cycles more.
+__device__ __forceinline__ bool elected() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.b32 %0, 1, 0, p;\n}" : "=r"(r));
+  return r;
+}
+
+// The staging area of an epilogue warp holds 32 rows of 64 entries in two parts, each as a box in the 128-byte swizzle of the
+// bulk copies: 16-byte piece c of row r lies at r * 128 + (c ^ r % 8) * 16, so that 8 lanes of neighbouring rows touch all banks.
+__device__ __forceinline__ uint4 *piece(uint8_t *part, int r, int c) {
+  return reinterpret_cast<uint4 *>(part + r * 128 + ((c ^ (r & 7)) << 4));
+}
 
 __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8]) {
   const uint32_t u[4] = {v.x, v.y, v.z, v.w};
@@ -455,137 +490,134 @@ __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8]) {
   }
 }
 
-// 32 entries of a row, as fp16 and (where lo is not NULL) the rest as fp16 again
-__device__ __forceinline__ void store_pair(const float (&v)[32], __half *hi, __half *lo) {
+// 8 entries: as fp16 and, where a second part is kept, the rest as fp16 again
+template <bool PAIR>
+__device__ __forceinline__ void put(uint8_t *stage, int r, int c, const float *v) {
+  uint32_t h[4], l[4];
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    uint32_t h[4], l[4];
+  for (int i = 0; i < 4; ++i) {
+    const __half2 hh = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+    h[i] = *reinterpret_cast<const uint32_t *>(&hh);
+    if constexpr (PAIR) {
+      const float2 f = __half22float2(hh);
+      const __half2 ll = __floats2half2_rn(v[2 * i] - f.x, v[2 * i + 1] - f.y);
+      l[i] = *reinterpret_cast<const uint32_t *>(&ll);
+    }
+  }
+  *piece(stage, r, c) = make_uint4(h[0], h[1], h[2], h[3]);
+  if constexpr (PAIR) *piece(stage + kStagePart, r, c) = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void get(uint8_t *stage, int r, int c, float (&x)[8]) {
+  unpack(*piece(stage, r, c), x);
+  if constexpr (PAIR) {
+    float y[8];
+    unpack(*piece(stage + kStagePart, r, c), y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] += y[i];
+  }
+}
+
+// The finished directions of 32 rows by 64 columns, through the staging area so that the stores to the caller's array, whose
+// rows need not be aligned, are of neighbouring elements.
+template <typename Out>
+__device__ __forceinline__ void write_out(const Plan &p, const Tile &t, uint8_t *stage, int lane, int row0, int col0, const float (&v)[64], Out *out, int vec) {
+  const Group &g = *t.g;
+  const float s = p.scale[g.m0 + t.z / p.K] * kUnstore;
+  __syncwarp();  // every lane has read its part of the area
+  constexpr int kPieces = 64 * sizeof(Out) / 16, kEach = 16 / sizeof(Out);
+  auto at = [&](int r, int c) { return reinterpret_cast<uint4 *>(stage + r * (64 * sizeof(Out)) + (((c & ~7) | ((c ^ r) & 7)) << 4)); };
+#pragma unroll
+  for (int c = 0; c < kPieces; ++c) {
+    uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float a = v[8 * q + 2 * i], b = v[8 * q + 2 * i + 1];
-      const __half ha = __float2half_rn(a), hb = __float2half_rn(b);
-      h[i] = pack_half(ha, hb);
-      l[i] = pack_half(__float2half_rn(a - __half2float(ha)), __float2half_rn(b - __half2float(hb)));
+      if constexpr (sizeof(Out) == 4) {
+        u[i] = __float_as_uint(v[4 * c + i] * s);
+      } else {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[8 * c + 2 * i] * s, v[8 * c + 2 * i + 1] * s);
+        u[i] = *reinterpret_cast<const uint32_t *>(&h);
+      }
     }
-    *reinterpret_cast<uint4 *>(hi + 8 * q) = make_uint4(h[0], h[1], h[2], h[3]);
-    if (lo) *reinterpret_cast<uint4 *>(lo + 8 * q) = make_uint4(l[0], l[1], l[2], l[3]);
+    *at(lane, c) = make_uint4(u[0], u[1], u[2], u[3]);
   }
+  __syncwarp();
+  Out *base = out + (t.z % p.K) * p.ld + p.offset[g.m0 + t.z / p.K] + (long long)row0 * g.cols + col0;
+  const int rows = min(kStageRows, g.rows - row0), cols = min(64, g.cols - col0);
+  if (vec && g.even == 2) {
+    constexpr int kAtOnce = 32 / kPieces;  // rows
+    const int c = lane % kPieces;
+#pragma unroll 4
+    for (int r = lane / kPieces; r < rows; r += kAtOnce)
+      if (c * kEach < cols) *reinterpret_cast<uint4 *>(base + (long long)r * g.cols + c * kEach) = *at(r, c);
+  } else {
+    for (int r = 0; r < rows; ++r)
+#pragma unroll
+      for (int e = lane; e < 64; e += 32)
+        if (e < cols) base[(long long)r * g.cols + e] = reinterpret_cast<const Out *>(at(r, e / kEach))[e % kEach];
+  }
+  __syncwarp();
 }
 
-// 32 entries of a row of a stored pair (or of its leading half)
-__device__ __forceinline__ void load_pair(const __half *hi, const __half *lo, float (&v)[32]) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    float x[8];
-    unpack(__ldcg(reinterpret_cast<const uint4 *>(hi + 8 * q)), x);
-    if (lo) {
-      float y[8];
-      unpack(__ldcg(reinterpret_cast<const uint4 *>(lo + 8 * q)), y);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] += y[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[8 * q + i] = x[i];
-  }
-}
-
-// One row's 32 columns of a finished tile.  row < the padded rows; stores are masked to the matrix.
+// 64 columns of the warp's 32 rows of a finished tile, from the accumulators in v to the staging area (or to the caller's
+// array, when the step is the last).  The area holds the entries of O (square) or X (update) that belong there.
 template <bool SPLIT, typename Out>
-__device__ __forceinline__ void finish(const Plan &p, const Tile &t, int row, int col, float (&acc)[32], Out *out, int vec) {
+__device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *stage, const float *columns, int lane, int row0, int col0, float (&v)[64],
+                                       Out *out, int vec) {
   const Group &g = *t.g;
-  const int z = t.z;
-  const long long zd = (long long)z * g.lda;
+  const long long zd = (long long)t.z * g.lda;
+  const int row = row0 + lane;
   if (t.phase != UPDATE) {
-    if (row >= g.lda || col >= g.lda) return;
-    const bool in = row < g.n, diag = t.ti == t.tj && (unsigned)(row - col) < 32u;
-    const long long at = ((long long)z * g.n + row) * g.lda + col;
-    float *d = t.phase == GRAM ? g.da : g.db;
+    const bool diag = t.ti == t.tj && row0 < col0 + 64 && col0 < row0 + 32;
     if (t.phase == GRAM) {
       if (diag) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (col + i == row) d[zd + row] = acc[i] * kUnstore2, acc[i] = 0.f;
+        for (int i = 0; i < 64; ++i)
+          if (col0 + i == row) {
+            if (row < g.lda) g.da[zd + row] = v[i] * kUnstore2;
+            v[i] = 0.f;
+          }
       }
 #pragma unroll
-      for (int i = 0; i < 32; ++i) acc[i] *= kUnstore;
-      if (in) store_pair(acc, g.a[0] + at, SPLIT ? g.a[1] + at : nullptr);
+      for (int i = 0; i < 64; ++i) v[i] *= kUnstore;
     } else {
       const float b = p.coef[t.it][1], c = p.coef[t.it][2];
-      float o[32] = {};
-      if (in) load_pair(g.a[0] + at, SPLIT ? g.a[1] + at : nullptr, o);
-      const float di = __ldcg(g.da + zd + row);
-      const float4 *dj = reinterpret_cast<const float4 *>(g.da + zd + col);
+      const float di = row < g.lda ? __ldcg(g.da + zd + row) : 0.f, cs = c * kUnstore;
+      if (diag) {
+#pragma unroll
+        for (int i = 0; i < 64; ++i)
+          if (col0 + i == row) {
+            if (row < g.lda) g.db[zd + row] = fmaf(di, fmaf(c, di, b), v[i] * c * kUnstore2);
+            v[i] = 0.f;  // and O_ii is zero
+          }
+      }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        const float4 v = __ldcg(dj + q);
-        const float w[4] = {v.x, v.y, v.z, v.w};
+        float o[8];
+        get<SPLIT>(stage, lane, q, o);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = 4 * q + i;
-          const float s = c * acc[e] * kUnstore;              // c (O^2)_ij, times kStore
-          if (diag && col + e == row) {
-            d[zd + row] = fmaf(di, fmaf(c, di, b), s * kUnstore);
-            acc[e] = 0.f;
-          } else {
-            acc[e] = fmaf(fmaf(c, di + w[i], b), o[e], s);
-          }
-        }
+        for (int i = 0; i < 8; ++i) v[8 * q + i] = fmaf(fmaf(c, di + columns[8 * q + i], b), o[i], v[8 * q + i] * cs);
       }
-      if (in) store_pair(acc, g.b[0] + at, SPLIT ? g.b[1] + at : nullptr);
     }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) put<SPLIT>(stage, lane, q, v + 8 * q);
     return;
   }
-  if (row >= g.rows || col >= g.ldx) return;
   const float a = p.coef[t.it][0];
-  const long long at = ((long long)z * g.rows + row) * g.ldx + col;
-  const int cur = t.it & 1;
-  float x[32];
-  load_pair(g.x[cur][0] + at, g.x[cur][1] + at, x);
-  if (!g.flip) {
-    const float k = a + __ldcg(g.db + zd + row);
+  const float k = !g.flip && row < g.lda ? a + __ldcg(g.db + zd + row) : a;
 #pragma unroll
-    for (int i = 0; i < 32; ++i) acc[i] = fmaf(k, x[i], acc[i] * kUnstore);
-  } else {
-    const float4 *dj = reinterpret_cast<const float4 *>(g.db + zd + col);
+  for (int q = 0; q < 8; ++q) {
+    float x[8];
+    get<true>(stage, lane, q, x);
 #pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const float4 v = __ldcg(dj + q);
-      acc[4 * q] = fmaf(a + v.x, x[4 * q], acc[4 * q] * kUnstore);
-      acc[4 * q + 1] = fmaf(a + v.y, x[4 * q + 1], acc[4 * q + 1] * kUnstore);
-      acc[4 * q + 2] = fmaf(a + v.z, x[4 * q + 2], acc[4 * q + 2] * kUnstore);
-      acc[4 * q + 3] = fmaf(a + v.w, x[4 * q + 3], acc[4 * q + 3] * kUnstore);
-    }
+    for (int i = 0; i < 8; ++i) v[8 * q + i] = fmaf(g.flip ? k + columns[8 * q + i] : k, x[i], v[8 * q + i] * kUnstore);
   }
   if (t.it + 1 < p.steps) {
-    store_pair(acc, g.x[cur ^ 1][0] + at, g.x[cur ^ 1][1] + at);
-    return;
-  }
-  const float s = p.scale[g.m0 + z / p.K] * kUnstore;
-  Out *o = out + (z % p.K) * p.ld + p.offset[g.m0 + z / p.K] + (long long)row * g.cols + col;
-  if (vec && g.even == 2 && col + 32 <= g.cols) {
-    if constexpr (sizeof(Out) == 4) {
 #pragma unroll
-      for (int q = 0; q < 8; ++q)
-        reinterpret_cast<float4 *>(o)[q] = make_float4(acc[4 * q] * s, acc[4 * q + 1] * s, acc[4 * q + 2] * s, acc[4 * q + 3] * s);
-    } else {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t u[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(acc[8 * q + 2 * i] * s, acc[8 * q + 2 * i + 1] * s);
-          u[i] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        reinterpret_cast<uint4 *>(o)[q] = make_uint4(u[0], u[1], u[2], u[3]);
-      }
-    }
+    for (int q = 0; q < 8; ++q) put<true>(stage, lane, q, v + 8 * q);
   } else {
-#pragma unroll
-    for (int i = 0; i < 32; ++i)
-      if (col + i < g.cols) {
-        if constexpr (sizeof(Out) == 4) o[i] = acc[i] * s;
-        else o[i] = __float2bfloat16_rn(acc[i] * s);
-      }
+    write_out<Out>(p, t, stage, lane, row0, col0, v, out, vec);
   }
 }
 
@@ -596,10 +628,14 @@ __device__ __forceinline__ void finish(const Plan &p, const Tile &t, int row, in
 // every CTA is resident (cooperative launch) and tiles depend only on earlier ones, so the wait for them ends.
 template <int CG, bool SPLIT, typename Out>
 __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *out, int vec) {
-  extern __shared__ uint8_t raw[];
-  __shared__ Shared sh;
+  extern __shared__ __align__(1024) uint8_t raw[];
+  Shared &sh = *reinterpret_cast<Shared *>(raw);
   constexpr int kCols = 128 * CG;
-  const uint32_t slots = (smem_u32(raw) + 1023) & ~1023u;
+  const uint32_t slots = smem_u32(sh.slots);
+  if (slots & 1023) {  // the swizzles below need it; nothing has started yet
+    if (threadIdx.x == 0) atomicExch(p.error, 1);
+    return;
+  }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int rank = 0;
   if constexpr (CG == 2) asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
@@ -608,6 +644,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&sh.full[i]), 1), mbar_init(smem_u32(&sh.empty[i]), 1);
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.acc_full[i]), 1), mbar_init(smem_u32(&sh.acc_empty[i]), CG * kEpiWarps);
+    for (int i = 0; i < kEpiWarps; ++i) mbar_init(smem_u32(&sh.in[i]), 1);
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -623,42 +660,41 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   constexpr int kParts = SPLIT ? 2 : 1;
 
   if (warp == 0) {
-    if (lane == 0) {
-      int slot = 0;
-      uint32_t phase = 0;
-      bool ok = true;
-      for (int i = first; ok && walk.at(p, i, t); i += stride) {
-        if (!(ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)))) break;
-        fence_async();
-        Operand oa, ob;
-        operands<CG>(t, oa, ob);
-        const CUtensorMap *maps = p.maps + (t.g - p.groups) * MAPS;
-        const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
-        const int a0 = oa.t * kCols + rank * 128, b0 = ob.t * kCols + rank * 128;
-        for (int kb = 0; ok && kb < kbs; ++kb) {
-          const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    for (int i = first; ok && walk.at(p, i, t); i += stride) {
+      if (!(ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)))) break;
+      fence_async();
+      Operand oa, ob;
+      operands<CG>(t, oa, ob);
+      const CUtensorMap *maps = p.maps + (t.g - p.groups) * MAPS;
+      const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+      const int a0 = oa.t * kCols + rank * 128, b0 = ob.t * kCols + rank * 128;
+      for (int kb = 0; ok && kb < kbs; ++kb) {
+        const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
+        const int ax = at ? a0 : kb * kBox, ay = at ? kb * kBox : a0, bx = bt ? b0 : kb * kBox, by = bt ? kb * kBox : b0;
 #pragma unroll
-          for (int part = 0; part < kParts; ++part) {
-            if (!(ok = wait.bar(smem_u32(&sh.empty[slot]), phase ^ 1))) break;
+        for (int part = 0; part < kParts; ++part) {
+          if (!(ok = wait.bar(smem_u32(&sh.empty[slot]), phase ^ 1))) break;
+          if (elected()) {
             uint32_t full = smem_u32(&sh.full[slot]);
             if (rank == 0) mbar_expect(full, CG * kSlotBytes);
             if constexpr (CG == 2) full = mapped(full, 0);
             const uint32_t dst = slots + slot * kSlotBytes;
             const CUtensorMap *ma = maps + oa.map + part, *mb = maps + ob.map + part;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              if (at) tma_load<CG>(dst + h * kBoxBytes, ma, full, a0 + h * kBox, kb * kBox, t.z);
-              else tma_load<CG>(dst + h * kBoxBytes, ma, full, kb * kBox, a0 + h * kBox, t.z);
-              if (bt) tma_load<CG>(dst + (2 + h) * kBoxBytes, mb, full, b0 + h * kBox, kb * kBox, t.z);
-              else tma_load<CG>(dst + (2 + h) * kBoxBytes, mb, full, kb * kBox, b0 + h * kBox, t.z);
-            }
-            if (++slot == kSlots) slot = 0, phase ^= 1;
+            tma_load<CG>(dst, ma, full, ax, ay, t.z);
+            tma_load<CG>(dst + kBoxBytes, ma, full, at ? ax + kBox : ax, at ? ay : ay + kBox, t.z);
+            tma_load<CG>(dst + 2 * kBoxBytes, mb, full, bx, by, t.z);
+            tma_load<CG>(dst + 3 * kBoxBytes, mb, full, bt ? bx + kBox : bx, bt ? by : by + kBox, t.z);
           }
+          __syncwarp();
+          if (++slot == kSlots) slot = 0, phase ^= 1;
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       int slot = 0, n = 0;
       uint32_t phase = 0;
       bool ok = true;
@@ -684,52 +720,103 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t src = slots + slot * kSlotBytes;
             da[part] = descriptor(src, at), db[part] = descriptor(src + 2 * kBoxBytes, bt), used[part] = slot;
-            if (part == 0) {
+            if (elected()) {
+              if (part == 0) {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[0] + k * sb, idesc, kb || k);
-            } else {
+                for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[0] + k * sb, idesc, kb || k);
+              } else {
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[kParts - 1] + k * sb, idesc, true);
+                for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[kParts - 1] + k * sb, idesc, true);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) mma<CG>(d, da[kParts - 1] + k * sa, db[0] + k * sb, idesc, true);
+                for (int k = 0; k < 4; ++k) mma<CG>(d, da[kParts - 1] + k * sa, db[0] + k * sb, idesc, true);
+              }
+              if (part == kParts - 1) {
+#pragma unroll
+                for (int u = 0; u < kParts; ++u) mma_commit<CG>(smem_u32(&sh.empty[used[u]]));
+                if (kb == kbs - 1) mma_commit<CG>(smem_u32(&sh.acc_full[acc]));
+              }
             }
+            __syncwarp();
             if (++slot == kSlots) slot = 0, phase ^= 1;
           }
-          if (ok) {
-#pragma unroll
-            for (int part = 0; part < kParts; ++part) mma_commit<CG>(smem_u32(&sh.empty[used[part]]));
-          }
         }
-        if (ok) mma_commit<CG>(smem_u32(&sh.acc_full[acc]));
       }
     }
   } else if (warp >= 4) {
     const int q = warp & 3, half = (warp - 4) >> 2;
+    uint8_t *stage = sh.stage[warp - 4];
+    float *columns = sh.columns[warp - 4];
+    const uint32_t in = smem_u32(&sh.in[warp - 4]), area = smem_u32(stage);
+    uint32_t in_phase = 0;
     int n = 0;
-    for (int i = first; walk.at(p, i, t); i += stride, ++n) {
+    bool ok = true;
+    for (int i = first; ok && walk.at(p, i, t); i += stride, ++n) {
       const int acc = n & 1;
-      // what the epilogue itself reads was finished by other CTAs: lane 0 acquires it for the warp
-      bool ok = true;
-      if (lane == 0) ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)) && wait.bar(smem_u32(&sh.acc_full[acc]), n >> 1 & 1);
-      if (!__shfl_sync(0xffffffffu, ok, 0)) break;
-      __syncwarp();
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int row = t.ti * kCols + rank * 128 + q * 32 + lane;
+      const Group &g = *t.g;
+      // what the epilogue itself reads was finished by other CTAs: it acquires that too
+      if (!(ok = wait.count(p.done + g.z0 + t.z, needed<CG>(t)))) break;
+      const bool update = t.phase == UPDATE, last = update && t.it + 1 == p.steps;
+      const int rows = update ? g.rows : g.n, cols = update ? g.cols : g.n;
+      const int row0 = t.ti * kCols + rank * 128 + q * 32;
+      const CUtensorMap *maps = p.maps + (t.g - p.groups) * MAPS + MAP_EPI;
+      const int parts = update ? 2 : kParts, take = t.phase == GRAM ? 0 : parts;
+      const CUtensorMap *from = maps + (update ? MAP_X + 2 * (t.it & 1) : MAP_A);
+      const CUtensorMap *to = maps + (update ? MAP_X + 2 * (t.it & 1 ^ 1) : t.phase == GRAM ? MAP_A : MAP_B);
+      const float *other = t.phase == SQUARE ? g.da : update && g.flip ? g.db : nullptr;
 #pragma unroll 1
-      for (int c = half * (kCols / 2); c < (half + 1) * (kCols / 2); c += 32) {
-        float v[32];
+      for (int u = 0; ok && u < CG; ++u) {
+        const int cw = half * (kCols / 2) + u * 64, col0 = t.tj * kCols + cw;
+        const bool live = row0 < rows && col0 < cols;
+        if (live && take) {  // while the products run
+          if (elected()) {
+            stores_read();   // the area's previous contents have left
+            fence_async();
+            mbar_expect(in, take * kStagePart);
+            for (int part = 0; part < take; ++part) tma_load<1>(area + part * kStagePart, from + part, in, col0, row0, t.z);
+          }
+          if (other) {
+            columns[lane] = col0 + lane < g.lda ? __ldcg(other + (long long)t.z * g.lda + col0 + lane) : 0.f;
+            columns[lane + 32] = col0 + lane + 32 < g.lda ? __ldcg(other + (long long)t.z * g.lda + col0 + lane + 32) : 0.f;
+          }
+        } else if (live) {
+          if (elected()) stores_read();
+        }
         __syncwarp();
-        tmem_load32(tmem + ((uint32_t)(q * 32) << 16) + acc * kCols + c, v);
-        finish<SPLIT, Out>(p, t, row, t.tj * kCols + c, v, out, vec);
+        if (u == 0) {
+          if (!(ok = wait.bar(smem_u32(&sh.acc_full[acc]), n >> 1 & 1))) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        }
+        float v[64];
+        tmem_load64(tmem + ((uint32_t)(q * 32) << 16) + acc * kCols + cw, v);
+        if (u == CG - 1) {  // the accumulator is free for the tile after next
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (elected()) mbar_arrive(smem_u32(&sh.acc_empty[acc]), 0);
+        }
+        if (!live) continue;
+        if (take) {
+          if (!(ok = wait.bar(in, in_phase))) break;
+          in_phase ^= 1;
+        }
+        finish<SPLIT, Out>(p, t, stage, columns, lane, row0, col0, v, out, vec);
+        if (!last) {
+          fence_async();  // what the lanes wrote is read by the bulk store
+          __syncwarp();
+          if (elected()) {
+            for (int part = 0; part < parts; ++part) tma_store(to + part, area + part * kStagePart, col0, row0, t.z);
+            stores_commit();
+          }
+        }
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      fence_async();  // the stores above are read by bulk copies
       __syncwarp();
-      if (lane == 0) {
-        mbar_arrive(smem_u32(&sh.acc_empty[acc]), 0);
-        add_release(p.done + t.g->z0 + t.z, 1);
+      if (ok && elected()) {
+        stores_done();
+        fence_async();
+        add_release(p.done + g.z0 + t.z, 1);
       }
+      __syncwarp();
     }
+    if (elected()) stores_done();
   }
   __syncwarp();
   __syncthreads();
@@ -940,12 +1027,17 @@ EncodeTiled encoder() {
   return reinterpret_cast<EncodeTiled>(f);
 }
 
-bool encode(EncodeTiled enc, CUtensorMap *map, void *base, int rows, int cols, int ld, int batch) {
+bool encode_box(EncodeTiled enc, CUtensorMap *map, void *base, int rows, int cols, int ld, int batch, int box_rows) {
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
   const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)rows * ld * 2};
-  const cuuint32_t box[3] = {kBox, kBox, 1}, step[3] = {1, 1, 1};
+  const cuuint32_t box[3] = {kBox, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, base, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// the box of the products' operands, and of the epilogues
+bool encode(EncodeTiled enc, CUtensorMap *map, void *base, int rows, int cols, int ld, int batch) {
+  return encode_box(enc, map, base, rows, cols, ld, batch, kBox) && encode_box(enc, map + MAP_EPI, base, rows, cols, ld, batch, kStageRows);
 }
 
 template <typename F>
@@ -957,7 +1049,7 @@ dasgd_status with_kernel(int cg, int dtype, F f) {
 
 void launch_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&attr)[2], int cg, int grid, cudaStream_t s) {
   lc = cudaLaunchConfig_t{};
-  lc.gridDim = dim3(grid), lc.blockDim = dim3(kThreads), lc.dynamicSmemBytes = kSmemBytes, lc.stream = s;
+  lc.gridDim = dim3(grid), lc.blockDim = dim3(kThreads), lc.dynamicSmemBytes = (int)sizeof(Shared), lc.stream = s;
   attr[0].id = cudaLaunchAttributeCooperative, attr[0].val.cooperative = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
   attr[1].val.clusterDim.x = cg, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
@@ -1063,7 +1155,7 @@ dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, 
 
   int sms = 0, clusters = 0;
   st = with_kernel(cg, c.dtype, [&](auto kernel, auto *) -> dasgd_status {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes);
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c.device);
     if (e == cudaSuccess && cg == 2) {
       cudaLaunchConfig_t lc;
