@@ -56,21 +56,26 @@ enum { GRAM = 0, SQUARE = 1, UPDATE = 2 };
 enum { MAP_X = 0, MAP_A = 4, MAP_B = 6, MAP_EPI = 8, MAPS = 16 };  // MAP_X + 2 * buffer + part; MAP_A + part; MAP_B + part; + MAP_EPI: the
                                                                    // same arrays in the epilogues' boxes of 32 rows
 
-struct Group {                                            // matrices of one shape, all replicas
+struct Shape {                                            // matrices of one shape, all replicas: what the products need
   int rows, cols, n, w, flip;                             // n = the smaller side; flip: n is the columns
-  int matrices, batch;                                    // batch = matrices * K, index z = matrix * K + replica
+  int batch;                                              // matrices * K, index z = matrix * K + replica
   int tn, tw, tg, tu;                                     // tiles of the sides; tiles of a symmetric product, of an update
   int even;                                               // 1: every matrix starts on a multiple of 8 elements of a row; 2: and has rows of such lengths
-  int ldx, lda;                                           // row strides (elements) of X and of A, B
-  int z0, m0;                                             // first matrix-of-a-replica, first matrix, over all groups
+  int lda;                                                // row stride (elements) of A and B, length of their diagonals
+  int z0, m0;                                             // first matrix-of-a-replica, first matrix, over all shapes
+  float *da, *db;                                         // diagonals of A and B, [batch][lda]
+};
+
+struct Group : Shape {                                    // and the kernels before them
+  int matrices, ldx;                                      // row stride (elements) of X
   int chunks, chunk0;                                     // pieces of a matrix in the momentum kernel; first piece of the group
   int rblk, rblks, rblk0;                                 // rows of a piece, pieces, first piece in the scaling kernel
   __half *x[2][2], *a[2], *b[2];                          // [buffer][part], [part]
-  float *da, *db;                                         // diagonals of A and B, [batch][lda]
 };
 
 struct Plan {                                             // kernel argument
   const Group *groups;
+  const Shape *shapes;                                    // the same, packed
   const CUtensorMap *maps;                                // [groups][MAPS]
   const long long *offset;                                // [matrices]
   const float *scale;                                     // [matrices]
@@ -273,7 +278,9 @@ __device__ __forceinline__ void add_release(unsigned *p, unsigned v) {
   asm volatile("red.release.gpu.global.add.u32 [%0], %1;" ::"l"(p), "r"(v) : "memory");
 }
 
-__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// between accesses of threads and of bulk copies: to device memory, to the CTA's shared memory
+__device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 template <int CG>
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap *map, uint32_t bar, int x, int y, int z) {
@@ -368,19 +375,20 @@ __device__ __forceinline__ uint64_t desc_step(bool outer) { return outer ? 2048 
 // tiles before it, and with several matrices the ones it depends on were finished long ago.
 struct Tile {
   int it, phase, z, ti, tj;
-  const Group *g;
+  const Shape *g;
+  int gi;  // the shape's index
 };
 
-template <int CG>
 struct Walk {
+  const Shape *shapes;
   int it = 0, phase = 0, g = 0, seg0 = 0;
   __device__ bool at(const Plan &p, int t, Tile &o) {
     for (;;) {
       if (it >= p.steps) return false;
-      const Group &gr = p.groups[g];
+      const Shape &gr = shapes[g];
       const int per = phase == UPDATE ? gr.tu : gr.tg, local = t - seg0;
       if (local < per * gr.batch) {
-        o.it = it, o.phase = phase, o.g = &gr, o.z = local / per;
+        o.it = it, o.phase = phase, o.g = &gr, o.gi = g, o.z = local / per;
         int r = local - o.z * per;
         if (phase == UPDATE) {
           const int tr = gr.flip ? gr.tw : gr.tn;
@@ -427,11 +435,14 @@ __device__ __forceinline__ bool outer(const Operand &o, int kb) {  // whether th
   return o.kind == 1 || (o.kind == 2 && kb / (2 * CG) < o.t);
 }
 
+constexpr int kSharedShapes = 8;  // more are read from device memory
+
 struct Shared {
   uint8_t slots[kSlots][kSlotBytes];
   uint8_t stage[kEpiWarps][kStage];
   float columns[kEpiWarps][64];          // what an epilogue warp needs of the other side's diagonal
   uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2], in[kEpiWarps];
+  Shape shapes[kSharedShapes];
   uint32_t tmem;
   volatile int abort;
 };
@@ -523,7 +534,7 @@ __device__ __forceinline__ void get(uint8_t *stage, int r, int c, float (&x)[8])
 // rows need not be aligned, are of neighbouring elements.
 template <typename Out>
 __device__ __forceinline__ void write_out(const Plan &p, const Tile &t, uint8_t *stage, int lane, int row0, int col0, const float (&v)[64], Out *out, int vec) {
-  const Group &g = *t.g;
+  const Shape &g = *t.g;
   const float s = p.scale[g.m0 + t.z / p.K] * kUnstore;
   __syncwarp();  // every lane has read its part of the area
   constexpr int kPieces = 64 * sizeof(Out) / 16, kEach = 16 / sizeof(Out);
@@ -560,37 +571,40 @@ __device__ __forceinline__ void write_out(const Plan &p, const Tile &t, uint8_t 
   __syncwarp();
 }
 
+// v[e], with a zero left in its place.  Selects, not a branch for each of 64 places: those cost 20,000 cycles.
+__device__ __forceinline__ float take_out(float (&v)[64], int e) {
+  float d = 0.f;
+#pragma unroll
+  for (int i = 0; i < 64; ++i) {
+    d = i == e ? v[i] : d;
+    v[i] = i == e ? 0.f : v[i];
+  }
+  return d;
+}
+
 // 64 columns of the warp's 32 rows of a finished tile, from the accumulators in v to the staging area (or to the caller's
 // array, when the step is the last).  The area holds the entries of O (square) or X (update) that belong there.
 template <bool SPLIT, typename Out>
-__device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *stage, const float *columns, int lane, int row0, int col0, float (&v)[64],
-                                       Out *out, int vec) {
-  const Group &g = *t.g;
+__device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *stage, const float *columns, float mine, int lane, int row0, int col0,
+                                       float (&v)[64], Out *out, int vec) {
+  const Shape &g = *t.g;
   const long long zd = (long long)t.z * g.lda;
   const int row = row0 + lane;
   if (t.phase != UPDATE) {
     const bool diag = t.ti == t.tj && row0 < col0 + 64 && col0 < row0 + 32;
     if (t.phase == GRAM) {
       if (diag) {
-#pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (col0 + i == row) {
-            if (row < g.lda) g.da[zd + row] = v[i] * kUnstore2;
-            v[i] = 0.f;
-          }
+        const float d = take_out(v, row - col0);
+        if ((unsigned)(row - col0) < 64u && row < g.lda) g.da[zd + row] = d * kUnstore2;
       }
 #pragma unroll
       for (int i = 0; i < 64; ++i) v[i] *= kUnstore;
     } else {
       const float b = p.coef[t.it][1], c = p.coef[t.it][2];
-      const float di = row < g.lda ? __ldcg(g.da + zd + row) : 0.f, cs = c * kUnstore;
-      if (diag) {
-#pragma unroll
-        for (int i = 0; i < 64; ++i)
-          if (col0 + i == row) {
-            if (row < g.lda) g.db[zd + row] = fmaf(di, fmaf(c, di, b), v[i] * c * kUnstore2);
-            v[i] = 0.f;  // and O_ii is zero
-          }
+      const float di = mine, cs = c * kUnstore;
+      if (diag) {  // O_ii is zero, so zero is left
+        const float d = take_out(v, row - col0);
+        if ((unsigned)(row - col0) < 64u && row < g.lda) g.db[zd + row] = fmaf(di, fmaf(c, di, b), d * c * kUnstore2);
       }
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
@@ -605,7 +619,7 @@ __device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *st
     return;
   }
   const float a = p.coef[t.it][0];
-  const float k = !g.flip && row < g.lda ? a + __ldcg(g.db + zd + row) : a;
+  const float k = a + mine;
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
     float x[8];
@@ -648,6 +662,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  const Shape *shapes = sh.shapes;
+  if (p.n_groups <= kSharedShapes) {
+    for (int i = threadIdx.x; i < p.n_groups; i += kThreads) sh.shapes[i] = p.groups[i];
+  } else {
+    shapes = p.shapes;
+  }
   if (warp == 2) tmem_alloc<CG>(smem_u32(&sh.tmem), 2 * kCols);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
@@ -655,7 +675,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sh.tmem;
   Patience wait{&sh.abort, p.error, p.timeout_ns};
-  Walk<CG> walk;
+  Walk walk{shapes};
   Tile t;
   constexpr int kParts = SPLIT ? 2 : 1;
 
@@ -665,10 +685,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     bool ok = true;
     for (int i = first; ok && walk.at(p, i, t); i += stride) {
       if (!(ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)))) break;
-      fence_async();
+      fence_async_global();
       Operand oa, ob;
       operands<CG>(t, oa, ob);
-      const CUtensorMap *maps = p.maps + (t.g - p.groups) * MAPS;
+      const CUtensorMap *maps = p.maps + t.gi * MAPS;
       const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
       const int a0 = oa.t * kCols + rank * 128, b0 = ob.t * kCols + rank * 128;
       for (int kb = 0; ok && kb < kbs; ++kb) {
@@ -752,17 +772,20 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     bool ok = true;
     for (int i = first; ok && walk.at(p, i, t); i += stride, ++n) {
       const int acc = n & 1;
-      const Group &g = *t.g;
+      const Shape &g = *t.g;
       // what the epilogue itself reads was finished by other CTAs: it acquires that too
       if (!(ok = wait.count(p.done + g.z0 + t.z, needed<CG>(t)))) break;
       const bool update = t.phase == UPDATE, last = update && t.it + 1 == p.steps;
       const int rows = update ? g.rows : g.n, cols = update ? g.cols : g.n;
       const int row0 = t.ti * kCols + rank * 128 + q * 32;
-      const CUtensorMap *maps = p.maps + (t.g - p.groups) * MAPS + MAP_EPI;
+      const CUtensorMap *maps = p.maps + t.gi * MAPS + MAP_EPI;
       const int parts = update ? 2 : kParts, take = t.phase == GRAM ? 0 : parts;
       const CUtensorMap *from = maps + (update ? MAP_X + 2 * (t.it & 1) : MAP_A);
       const CUtensorMap *to = maps + (update ? MAP_X + 2 * (t.it & 1 ^ 1) : t.phase == GRAM ? MAP_A : MAP_B);
+      // the diagonal's entries of the tile's columns, and of this lane's row
       const float *other = t.phase == SQUARE ? g.da : update && g.flip ? g.db : nullptr;
+      const float *own = t.phase == SQUARE ? g.da : update && !g.flip ? g.db : nullptr;
+      const float mine = own && row0 + lane < g.lda ? __ldcg(own + (long long)t.z * g.lda + row0 + lane) : 0.f;
 #pragma unroll 1
       for (int u = 0; ok && u < CG; ++u) {
         const int cw = half * (kCols / 2) + u * 64, col0 = t.tj * kCols + cw;
@@ -770,7 +793,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
         if (live && take) {  // while the products run
           if (elected()) {
             stores_read();   // the area's previous contents have left
-            fence_async();
+            fence_async_global();
+            fence_async_shared();
             mbar_expect(in, take * kStagePart);
             for (int part = 0; part < take; ++part) tma_load<1>(area + part * kStagePart, from + part, in, col0, row0, t.z);
           }
@@ -798,9 +822,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
           if (!(ok = wait.bar(in, in_phase))) break;
           in_phase ^= 1;
         }
-        finish<SPLIT, Out>(p, t, stage, columns, lane, row0, col0, v, out, vec);
+        finish<SPLIT, Out>(p, t, stage, columns, mine, lane, row0, col0, v, out, vec);
         if (!last) {
-          fence_async();  // what the lanes wrote is read by the bulk store
+          fence_async_shared();  // what the lanes wrote is read by the bulk store
           __syncwarp();
           if (elected()) {
             for (int part = 0; part < parts; ++part) tma_store(to + part, area + part * kStagePart, col0, row0, t.z);
@@ -810,8 +834,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       }
       __syncwarp();
       if (ok && elected()) {
-        stores_done();
-        fence_async();
+        stores_done();  // visible to this thread, and by the release to those that acquire
         add_release(p.done + g.z0 + t.z, 1);
       }
       __syncwarp();
@@ -897,7 +920,7 @@ struct Layout {
   std::vector<float> scale;
   int chunks = 0, rblks = 0;
   long long n_done = 0, most_tiles = 0;
-  size_t groups_at, maps_at, offset_at, scale_at, done_at, sumsq_at, error_at, tables, bytes;
+  size_t groups_at, shapes_at, maps_at, offset_at, scale_at, done_at, sumsq_at, error_at, tables, bytes;
 };
 
 dasgd_status layout(const dasgd_ortho_config *c, const char *who, int cg, Layout &o) {
@@ -911,7 +934,7 @@ dasgd_status layout(const dasgd_ortho_config *c, const char *who, int cg, Layout
     if (g == o.groups.size()) {
       o.groups.emplace_back();
       Group &n = o.groups.back();
-      memset(&n, 0, sizeof n);
+      n = Group{};
       n.rows = m.rows, n.cols = m.cols;
       members.emplace_back();
     }
@@ -957,6 +980,7 @@ dasgd_status layout(const dasgd_ortho_config *c, const char *who, int cg, Layout
   if (tiles_all * kMaxSteps >= (1LL << 31) || z0 >= (1LL << 30)) return unsupported(at + "too many or too large matrices for one call");
   o.chunks = (int)chunks, o.rblks = (int)rblks, o.n_done = z0;
   o.groups_at = take(o.groups.size() * sizeof(Group));
+  o.shapes_at = take(o.groups.size() * sizeof(Shape));
   o.maps_at = take(o.groups.size() * MAPS * sizeof(CUtensorMap));
   o.offset_at = take(o.offset.size() * 8), o.scale_at = take(o.scale.size() * 4);
   o.error_at = take(4);
@@ -1013,7 +1037,20 @@ void coefficients(const dasgd_ortho_config *c, int &steps, float (*coef)[3]) {
     for (int j = 0; j < 3; ++j) coef[i][j] = c->coefficients ? c->coefficients[3 * i + j] : kDefaultCoef[j];
 }
 
-int choose_tile(const dasgd_ortho_config *c) { return c->tile ? c->tile / 128 : 1; }
+// CTAs of a tile.  Pairs of CTAs on 256-wide tiles read half as much per operation, single CTAs on 128-wide tiles put four
+// times as many SMs to work.  A tile's loop is bound by what an SM can take in (53 to 60 bytes a cycle), so pairs win as soon as
+// the updates' tiles nearly fill the 74 pairs: one 2048^2 (64 tiles) 402 us against 484 in bfloat16, a block of width 1024
+// (96 tiles) 522 against 630; below that single CTAs: one 1024^2 (16 tiles) 233 us against 258, eight 512^2 (32 tiles) 194
+// against 214.  In float32: 809 / 811, 912 / 1105, 365 / 469, 272 / 336.
+constexpr long long kEnoughTiles = 64;
+
+int choose_tile(const dasgd_ortho_config *c) {
+  if (c->tile) return c->tile / 128;
+  long long tiles = 0;
+  for (int i = 0; i < c->n_matrices; ++i)
+    tiles += (long long)((c->matrices[i].rows + 255) / 256) * ((c->matrices[i].cols + 255) / 256);
+  return tiles * c->K >= kEnoughTiles ? 2 : 1;
+}
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -1139,13 +1176,18 @@ dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, 
     at(g.da), at(g.db);
   }
   memcpy(host.data() + l.groups_at, l.groups.data(), l.groups.size() * sizeof(Group));
+  for (size_t i = 0; i < l.groups.size(); ++i) {
+    const Shape &shape = l.groups[i];
+    memcpy(host.data() + l.shapes_at + i * sizeof(Shape), &shape, sizeof shape);
+  }
   memcpy(host.data() + l.offset_at, l.offset.data(), l.offset.size() * 8);
   memcpy(host.data() + l.scale_at, l.scale.data(), l.scale.size() * 4);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((e = cudaMemcpyAsync(ws, host.data(), l.tables, cudaMemcpyHostToDevice, s)) != cudaSuccess || (e = cudaStreamSynchronize(s)) != cudaSuccess)
     return cuda_fail(e, "ortho_init");
 
-  p.groups = reinterpret_cast<const Group *>(ws + l.groups_at), p.maps = reinterpret_cast<const CUtensorMap *>(ws + l.maps_at);
+  p.groups = reinterpret_cast<const Group *>(ws + l.groups_at), p.shapes = reinterpret_cast<const Shape *>(ws + l.shapes_at);
+  p.maps = reinterpret_cast<const CUtensorMap *>(ws + l.maps_at);
   p.offset = reinterpret_cast<const long long *>(ws + l.offset_at), p.scale = reinterpret_cast<const float *>(ws + l.scale_at);
   p.done = reinterpret_cast<unsigned *>(ws + l.done_at), p.sumsq = reinterpret_cast<double *>(ws + l.sumsq_at);
   p.error = reinterpret_cast<int *>(ws + l.error_at);
