@@ -16,7 +16,10 @@
 //       A = D + O:  A^2_ij = (O^2)_ij + O_ij (D_i + D_j), A^2_ii = (O^2)_ii + D_i^2;   BX = diag(B) X + off(B) X;
 //   - only off-diagonal parts and the leading half of X enter products ("half" operands, for bfloat16 directions).  Their
 //     errors stay below the rounding of the output (2-norm, against 64 bits: 2e-4 to 1.3e-3, the rounding being 1.7e-3);
-//   - for float32 directions every operand is a pair and every product three (hi hi + hi lo + lo hi).
+//   - for float32 directions every operand is a pair and every product three (hi hi + hi lo + lo hi).  The tensor cores cut
+//     off what does not fit an accumulator, so long sums come out too small, by about 2e-8 of their size for every 16 terms
+//     of every product (1.8e-5 of the directions at 1024 x 4096): their accumulators are emptied every 256 terms into
+//     registers, where sums are rounded.
 // Everything in fp16 is stored times 2^12, so that pairs of entries of size 1/4096 stay clear of the subnormals; the host
 // refuses coefficients that could carry an entry past the largest fp16 number.
 #include "dasgd.h"
@@ -325,6 +328,22 @@ template <int CG>
 __device__ __forceinline__ void tmem_free(uint32_t addr, int cols) {
   if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+}
+
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {"
+      "%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,"
+      "%28,%29,%30,%31"
+      "}, [%32];\n tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]),
+        "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]),
+        "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(addr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
 __device__ __forceinline__ void tmem_load64(uint32_t addr, float (&v)[64]) {
@@ -637,6 +656,20 @@ __device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *st
 
 // ---------------------------------------------------------------- all products of all steps in one launch
 
+// Inner blocks of 64 that are summed in one accumulator: 256 terms where operands are pairs, all of them otherwise.
+template <bool SPLIT>
+__host__ __device__ constexpr int sum_blocks() { return SPLIT ? 4 : 1 << 30; }
+
+// Where an epilogue thread holds a row of a tile of 256 (pairs only), 128 sums need more than the 168 registers that 384
+// threads leave each other: the four warps that only issue give theirs up.  128 * 72 + 256 * 216 = 384 * 168.
+template <bool MORE, int N>
+__device__ __forceinline__ void registers() {
+  if constexpr (MORE) {
+    if constexpr (N > 168) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+  }
+}
+
 // CG CTAs work on a tile of 128 CG x 128 CG.  Warp 0 loads, warp 1 multiplies, warps 4 to 11 finish tiles; two accumulators
 // in tensor memory let the next tile's products run while a tile is finished.  CTA (or pair) q takes tiles q, q + Q, ...:
 // every CTA is resident (cooperative launch) and tiles depend only on earlier ones, so the wait for them ends.
@@ -677,8 +710,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   Patience wait{&sh.abort, p.error, p.timeout_ns};
   Walk walk{shapes};
   Tile t;
-  constexpr int kParts = SPLIT ? 2 : 1;
+  constexpr int kParts = SPLIT ? 2 : 1, kSum = sum_blocks<SPLIT>();
+  constexpr bool kMore = SPLIT && CG == 2;
 
+  if (warp < 4) registers<kMore, 72>();
   if (warp == 0) {
     int slot = 0;
     uint32_t phase = 0;
@@ -720,11 +755,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       bool ok = true;
       // float32 accumulators, fp16 operands, M = 128 CG, N = 128 CG
       const uint32_t shape = 1u << 4 | (uint32_t)(kCols >> 3) << 17 | (uint32_t)(kCols >> 4) << 24;
-      for (int i = first; ok && walk.at(p, i, t); i += stride, ++n) {
-        const int acc = n & 1;
-        if (!(ok = wait.bar(smem_u32(&sh.acc_empty[acc]), (n >> 1 & 1) ^ 1))) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem + acc * kCols;
+      for (int i = first; ok && walk.at(p, i, t); i += stride) {
         Operand oa, ob;
         operands<CG>(t, oa, ob);
         const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
@@ -734,6 +765,13 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
           const uint64_t sa = desc_step(at), sb = desc_step(bt);
           uint64_t da[kParts], db[kParts];
           int used[kParts];
+          const int acc = n & 1;
+          const uint32_t d = tmem + acc * kCols;
+          const bool fresh = kb % kSum == 0, full = kb == kbs - 1 || kb % kSum == kSum - 1;
+          if (fresh) {
+            if (!(ok = wait.bar(smem_u32(&sh.acc_empty[acc]), (n >> 1 & 1) ^ 1))) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          }
 #pragma unroll
           for (int part = 0; part < kParts; ++part) {
             if (!(ok = wait.bar(smem_u32(&sh.full[slot]), phase))) break;
@@ -743,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
             if (elected()) {
               if (part == 0) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[0] + k * sb, idesc, kb || k);
+                for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[0] + k * sb, idesc, !fresh || k);
               } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mma<CG>(d, da[0] + k * sa, db[kParts - 1] + k * sb, idesc, true);
@@ -753,16 +791,18 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
               if (part == kParts - 1) {
 #pragma unroll
                 for (int u = 0; u < kParts; ++u) mma_commit<CG>(smem_u32(&sh.empty[used[u]]));
-                if (kb == kbs - 1) mma_commit<CG>(smem_u32(&sh.acc_full[acc]));
+                if (full) mma_commit<CG>(smem_u32(&sh.acc_full[acc]));
               }
             }
             __syncwarp();
             if (++slot == kSlots) slot = 0, phase ^= 1;
           }
+          n += full;
         }
       }
     }
   } else if (warp >= 4) {
+    registers<kMore, 216>();
     const int q = warp & 3, half = (warp - 4) >> 2;
     uint8_t *stage = sh.stage[warp - 4];
     float *columns = sh.columns[warp - 4];
@@ -770,8 +810,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     uint32_t in_phase = 0;
     int n = 0;
     bool ok = true;
-    for (int i = first; ok && walk.at(p, i, t); i += stride, ++n) {
-      const int acc = n & 1;
+    for (int i = first; ok && walk.at(p, i, t); i += stride) {
       const Shape &g = *t.g;
       // what the epilogue itself reads was finished by other CTAs: it acquires that too
       if (!(ok = wait.count(p.done + g.z0 + t.z, needed<CG>(t)))) break;
@@ -786,40 +825,34 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       const float *other = t.phase == SQUARE ? g.da : update && g.flip ? g.db : nullptr;
       const float *own = t.phase == SQUARE ? g.da : update && !g.flip ? g.db : nullptr;
       const float mine = own && row0 + lane < g.lda ? __ldcg(own + (long long)t.z * g.lda + row0 + lane) : 0.f;
-#pragma unroll 1
-      for (int u = 0; ok && u < CG; ++u) {
-        const int cw = half * (kCols / 2) + u * 64, col0 = t.tj * kCols + cw;
-        const bool live = row0 < rows && col0 < cols;
-        if (live && take) {  // while the products run
+      const int colw = t.tj * kCols + half * (kCols / 2);  // the warp's columns: units of 64
+      const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16) + half * (kCols / 2);
+      // starts bringing in what is stored where unit u goes, and fetches the diagonal's entries of its columns
+      auto bring = [&](int u) {
+        const int col0 = colw + u * 64;
+        if (row0 < rows && col0 < cols) {
           if (elected()) {
-            stores_read();   // the area's previous contents have left
-            fence_async_global();
-            fence_async_shared();
-            mbar_expect(in, take * kStagePart);
-            for (int part = 0; part < take; ++part) tma_load<1>(area + part * kStagePart, from + part, in, col0, row0, t.z);
+            stores_read();  // the area's previous contents have left
+            if (take) {
+              fence_async_global();
+              fence_async_shared();
+              mbar_expect(in, take * kStagePart);
+              for (int part = 0; part < take; ++part) tma_load<1>(area + part * kStagePart, from + part, in, col0, row0, t.z);
+            }
           }
           if (other) {
             columns[lane] = col0 + lane < g.lda ? __ldcg(other + (long long)t.z * g.lda + col0 + lane) : 0.f;
             columns[lane + 32] = col0 + lane + 32 < g.lda ? __ldcg(other + (long long)t.z * g.lda + col0 + lane + 32) : 0.f;
           }
-        } else if (live) {
-          if (elected()) stores_read();
         }
         __syncwarp();
-        if (u == 0) {
-          if (!(ok = wait.bar(smem_u32(&sh.acc_full[acc]), n >> 1 & 1))) break;
-          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        }
-        float v[64];
-        tmem_load64(tmem + ((uint32_t)(q * 32) << 16) + acc * kCols + cw, v);
-        if (u == CG - 1) {  // the accumulator is free for the tile after next
-          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-          __syncwarp();
-          if (elected()) mbar_arrive(smem_u32(&sh.acc_empty[acc]), 0);
-        }
-        if (!live) continue;
+      };
+      // finishes unit u, whose sums are v
+      auto end = [&](int u, float (&v)[64]) {
+        const int col0 = colw + u * 64;
+        if (!(row0 < rows && col0 < cols)) return true;
         if (take) {
-          if (!(ok = wait.bar(in, in_phase))) break;
+          if (!wait.bar(in, in_phase)) return false;
           in_phase ^= 1;
         }
         finish<SPLIT, Out>(p, t, stage, columns, mine, lane, row0, col0, v, out, vec);
@@ -830,6 +863,52 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
             for (int part = 0; part < parts; ++part) tma_store(to + part, area + part * kStagePart, col0, row0, t.z);
             stores_commit();
           }
+        }
+        return true;
+      };
+      auto accumulated = [&]() {  // the accumulator that is due holds its sums
+        if (!wait.bar(smem_u32(&sh.acc_full[n & 1]), n >> 1 & 1)) return false;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        return true;
+      };
+      auto release = [&]() {      // it has been read
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (elected()) mbar_arrive(smem_u32(&sh.acc_empty[n & 1]), 0);
+        ++n;
+      };
+      bring(0);
+      if constexpr (SPLIT) {
+        float v[CG][64];
+        const int kbs = ((t.phase == GRAM ? g.w : g.n) + kBox - 1) / kBox;
+        for (int kb = 0; kb < kbs; kb += kSum) {
+          if (!(ok = accumulated())) break;
+#pragma unroll
+          for (int h = 0; h < 2 * CG; ++h) {
+            float x[32];
+            tmem_load32(lanes + (n & 1) * kCols + h * 32, x);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float &sum = v[h >> 1][(h & 1) * 32 + e];
+              sum = kb ? sum + x[e] : x[e];
+            }
+          }
+          release();
+        }
+#pragma unroll
+        for (int u = 0; u < CG; ++u) {
+          if (u && ok) bring(u);
+          if (ok) ok = end(u, v[u]);
+        }
+      } else {
+        if (!(ok = accumulated())) break;
+#pragma unroll 1
+        for (int u = 0; ok && u < CG; ++u) {
+          if (u) bring(u);
+          float v[64];
+          tmem_load64(lanes + (n & 1) * kCols + u * 64, v);
+          if (u == CG - 1) release();
+          ok = end(u, v);
         }
       }
       __syncwarp();
