@@ -28,28 +28,35 @@ constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kMaxRadixBits 
 
 // ---------------------------------------------------------------- loads and stores of VEC elements
 
+// VEC elements as they lie in memory.  Loading and widening are two steps: several rows are loaded before the first is
+// widened, and a load under a condition must not drag the widening, which waits for the data, into its branch.
 template <typename T, int VEC>
-__device__ __forceinline__ void load(const T *p, float (&x)[VEC]) {
-  if constexpr (VEC == 1) {
-    x[0] = static_cast<float>(__ldg(p));
-  } else if constexpr (sizeof(T) == 4) {
-    static_assert(VEC % 4 == 0, "16-byte accesses");
+struct Raw {
+  static constexpr int kWords = VEC * (int)sizeof(T) / 16;
+  uint4 w[kWords];
+  __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-    for (int i = 0; i < VEC / 4; ++i) {
-      const float4 v = __ldg(reinterpret_cast<const float4 *>(p) + i);
-      x[4 * i] = v.x, x[4 * i + 1] = v.y, x[4 * i + 2] = v.z, x[4 * i + 3] = v.w;
-    }
-  } else {
-    static_assert(VEC == 8, "16-byte accesses");
-    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+    for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+  }
+  __device__ __forceinline__ void widen(float (&x)[VEC]) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    for (int i = 0; i < kWords; ++i) {
+      const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 4) x[4 * i + j] = __uint_as_float(u[j]);
+        else x[8 * i + 2 * j] = __uint_as_float(u[j] << 16), x[8 * i + 2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+      }
     }
   }
-}
+};
+
+template <typename T>
+struct Raw<T, 1> {
+  T w;
+  __device__ __forceinline__ void load(const T *p) { w = __ldg(p); }
+  __device__ __forceinline__ void widen(float (&x)[1]) const { x[0] = static_cast<float>(w); }
+};
 
 __device__ __forceinline__ uint32_t pack(float a, float b) {
   const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
@@ -107,22 +114,17 @@ __global__ void __launch_bounds__(kThreads) k_embed_lookup(const LookupArgs a) {
     src[j] = table + (hit[j] ? tok : 0) * a.D;
   }
   for (int c = tx * VEC; c < a.D; c += X * VEC) {
-    float x[kRows][VEC];
+    Raw<W, VEC> raw[kRows];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-      if (hit[j]) {
-        load<W, VEC>(src[j] + c, x[j]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) x[j][i] = 0.f;
-      }
-    }
+    for (int j = 0; j < kRows; ++j) raw[j].load(src[j] + c);
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
       if (!live[j]) continue;
+      float x[VEC];
+      raw[j].widen(x);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[j][i] = hit[j] ? __fmul_rn(x[j][i], a.scale) : 0.f;
-      store<O, VEC>(out + (t0 + (long long)j * Y) * a.D + c, x[j]);
+      for (int i = 0; i < VEC; ++i) x[i] = hit[j] ? __fmul_rn(x[i], a.scale) : 0.f;
+      store<O, VEC>(out + (t0 + (long long)j * Y) * a.D + c, x);
     }
   }
 }
@@ -132,50 +134,94 @@ __global__ void __launch_bounds__(kThreads) k_embed_lookup(const LookupArgs a) {
 struct SortArgs {
   const void *tokens;
   uint32_t *key[2], *pos[2];  // [K][T] each; the sorted result is in [passes & 1]
-  uint8_t *met;               // [K][V]: 1 where the table's row is selected by some token
   long long T;
-  int V, token_bits, passes, radix_bits;
+  int V, token_bits, passes, radix_bits, K;
+  int sorted;                 // replicas to sort: K, or 0 without tokens
+  char *grad;                 // the table's gradient, to be zeroed; NULL: left alone
+  long long grad_stride, grad_bytes;  // from replica to replica, of a replica
 };
 
-// One cluster sorts one replica's tokens: a stable radix sort from the lowest digit up, `passes` digits of `radix_bits`
-// bits.  Every CTA owns a contiguous part of the sequence and every warp a contiguous part of that, so the order within
-// a digit is (CTA, warp, round, lane) = the order of the sequence.  Tokens outside the table get the key V and sort to
+constexpr int kZeroCtas = 148 * 3;    // with the sorting clusters in front they fill the SMs
+constexpr int kZeroPiece = 1 << 16;  // bytes that a CTA zeroes at a time
+
+__device__ __forceinline__ void zero_piece(char *p, int n) {  // n <= kZeroPiece bytes, an even number
+  const int head = min(n, (int)(-reinterpret_cast<uintptr_t>(p) & 15)), body = (n - head) / 16, tail = n - head - body * 16;
+  if (threadIdx.x < head / 2) reinterpret_cast<uint16_t *>(p)[threadIdx.x] = 0;
+  uint4 *q = reinterpret_cast<uint4 *>(p + head);
+#pragma unroll 8
+  for (int i = threadIdx.x; i < body; i += kSortThreads) __stcs(q + i, make_uint4(0, 0, 0, 0));
+  if (threadIdx.x < tail / 2) reinterpret_cast<uint16_t *>(q + body)[threadIdx.x] = 0;
+}
+
+// The first K clusters each sort one replica's tokens: a stable radix sort from the lowest digit up, `passes` digits of
+// `radix_bits` bits.  Every CTA owns a contiguous part of the sequence and every warp a contiguous part of that, so the order
+// within a digit is (CTA, warp, round, lane) = the order of the sequence.  Tokens outside the table get the key V and sort to
 // the end.  All passes run in one launch: the digit counts cross CTAs through distributed shared memory, the keys
-// through L2, and a cluster barrier (a fraction of a microsecond) stands where a launch boundary would.
+// through L2, and a cluster barrier (about a microsecond) stands where a launch boundary would.
+//
+// Sorting keeps a few SMs busy with latencies.  The clusters after the first K meanwhile zero the whole table of every replica
+// (rows that tokens select are written once more by the sums: cheaper than waiting to know which).
 __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) {
   __shared__ uint32_t hist[kSortWarps][kMaxRadix];
   __shared__ uint32_t total[kMaxRadix];
   __shared__ uint32_t scan[kSortThreads / 32];
+  asm volatile("griddepcontrol.launch_dependents;");
   cg::cluster_group cluster = cg::this_cluster();
   const int nC = cluster.num_blocks(), rank = cluster.block_rank();
   const long long k = blockIdx.x / nC;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (k >= a.sorted) {
+    const long long per = (a.grad_bytes + kZeroPiece - 1) / kZeroPiece, all = per * a.K;
+    for (long long i = blockIdx.x - (long long)a.sorted * nC; i < all; i += gridDim.x - (long long)a.sorted * nC) {
+      const long long at = i % per * kZeroPiece;
+      zero_piece(a.grad + i / per * a.grad_stride + at, (int)min((long long)kZeroPiece, a.grad_bytes - at));
+    }
+    return;
+  }
+  constexpr int kBatch = 8;  // keys of a lane that are loaded together
   const int R = 1 << a.radix_bits;
   const uint32_t none = (uint32_t)a.V;
-  const long long per = (a.T + nC - 1) / nC;                            // positions of a CTA
+  const long long per = (a.T + nC - 1) / nC;                                   // positions of a CTA
   const long long seg = ((per + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;  // positions of a warp
   const long long lo = min(a.T, rank * per), hi = min(a.T, lo + per);
   const long long w0 = min(hi, lo + warp * seg), w1 = min(hi, w0 + seg);
-  uint8_t *met = a.met + k * a.V;
-  for (long long v = rank * (long long)kSortThreads + tid; v < a.V; v += (long long)nC * kSortThreads) met[v] = 0;
 
   for (int pass = 0; pass < a.passes; ++pass) {
     const uint32_t *kin = a.key[pass & 1] + k * a.T, *pin = a.pos[pass & 1] + k * a.T;
     uint32_t *kout = a.key[(pass & 1) ^ 1] + k * a.T, *pout = a.pos[(pass & 1) ^ 1] + k * a.T;
     const int shift = pass * a.radix_bits;
-    auto key_at = [&](long long i) -> uint32_t {
-      if (pass) return __ldcg(kin + i);
-      const long long t = token_at(a.tokens, a.token_bits, k * a.T + i);
-      return t >= 0 && t < a.V ? (uint32_t)t : none;
+    uint32_t keys[kBatch];
+    auto load_keys = [&](long long base) {
+      if (pass) {
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) {
+          const long long i = base + r * 32 + lane;
+          keys[r] = i < w1 ? __ldcg(kin + i) : 0;
+        }
+      } else {
+        long long t[kBatch];
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) {
+          const long long i = base + r * 32 + lane;
+          t[r] = i < w1 ? token_at(a.tokens, a.token_bits, k * a.T + i) : 0;
+        }
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) keys[r] = t[r] >= 0 && t[r] < a.V ? (uint32_t)t[r] : none;
+      }
     };
     for (int d = lane; d < R; d += 32) hist[warp][d] = 0;
     __syncwarp();
-    for (long long i = w0 + lane; i - lane < w1; i += 32) {
-      const bool in = i < w1;
-      const uint32_t d = in ? (key_at(i) >> shift) & (R - 1) : (uint32_t)R;
-      const unsigned same = __match_any_sync(0xffffffffu, d);
-      if (in && lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
-      __syncwarp();
+    for (long long base = w0; base < w1; base += kBatch * 32) {
+      load_keys(base);
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        if (base + r * 32 >= w1) break;
+        const bool in = base + r * 32 + lane < w1;
+        const uint32_t d = in ? (keys[r] >> shift) & (R - 1) : (uint32_t)R;
+        const unsigned same = __match_any_sync(0xffffffffu, d);
+        if (in && lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
+        __syncwarp();
+      }
     }
     __syncthreads();
     if (tid < R) {  // counts of the warps -> exclusive prefix over the warps, and the CTA's total
@@ -191,10 +237,13 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
     cluster.sync();
     uint32_t before = 0, all = 0;
     if (tid < R) {
-      for (int c = 0; c < nC; ++c) {
-        const uint32_t n = *cluster.map_shared_rank(&total[tid], c);
-        all += n;
-        if (c < rank) before += n;
+      uint32_t n[8];  // a cluster has at most 8 CTAs
+#pragma unroll
+      for (int c = 0; c < 8; ++c) n[c] = c < nC ? *cluster.map_shared_rank(&total[tid], c) : 0;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        all += n[c];
+        if (c < rank) before += n[c];
       }
     }
     uint32_t incl = all;  // exclusive scan of `all` over the digits (threads beyond R hold 0)
@@ -205,32 +254,38 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
     }
     if (lane == 31) scan[warp] = incl;
     __syncthreads();
-    uint32_t base = incl - all + before;
-    for (int w = 0; w < warp; ++w) base += scan[w];
+    uint32_t base0 = incl - all + before;
+#pragma unroll
+    for (int w = 0; w < kSortWarps; ++w) base0 += w < warp ? scan[w] : 0;
     if (tid < R)
 #pragma unroll
-      for (int w = 0; w < kSortWarps; ++w) hist[w][tid] += base;
+      for (int w = 0; w < kSortWarps; ++w) hist[w][tid] += base0;
     __syncthreads();
-    for (long long i = w0 + lane; i - lane < w1; i += 32) {
-      const bool in = i < w1;
-      const uint32_t key = in ? key_at(i) : 0;
-      const uint32_t d = in ? (key >> shift) & (R - 1) : (uint32_t)R;
-      const unsigned same = __match_any_sync(0xffffffffu, d);
-      if (in) {
-        const uint32_t at = hist[warp][d] + __popc(same & ((1u << lane) - 1));
-        kout[at] = key;
-        pout[at] = pass ? __ldcg(pin + i) : (uint32_t)i;
+    for (long long base = w0; base < w1; base += kBatch * 32) {
+      load_keys(base);
+      uint32_t from[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        const long long i = base + r * 32 + lane;
+        from[r] = !pass ? (uint32_t)i : i < w1 ? __ldcg(pin + i) : 0;
       }
-      __syncwarp();
-      if (in && lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
-      __syncwarp();
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        if (base + r * 32 >= w1) break;
+        const bool in = base + r * 32 + lane < w1;
+        const uint32_t d = in ? (keys[r] >> shift) & (R - 1) : (uint32_t)R;
+        const unsigned same = __match_any_sync(0xffffffffu, d);
+        if (in) {
+          const uint32_t at = hist[warp][d] + __popc(same & ((1u << lane) - 1));
+          kout[at] = keys[r];
+          pout[at] = from[r];
+        }
+        __syncwarp();
+        if (in && lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
+        __syncwarp();
+      }
     }
     cluster.sync();  // the next pass reads what other CTAs wrote, and `total` may be overwritten
-  }
-  const uint32_t *key = a.key[a.passes & 1] + k * a.T;
-  for (long long i = lo + tid; i < hi; i += kSortThreads) {
-    const uint32_t v = __ldcg(key + i);
-    if (v != none && (i == 0 || __ldcg(key + i - 1) != v)) met[v] = 1;
   }
 }
 
@@ -240,39 +295,24 @@ struct GradArgs {
   const void *dy;             // [K][T][D]
   void *grad;                 // already moved to the table's first element
   const uint32_t *key, *pos;  // [K][T], sorted
-  const uint8_t *met;         // [K][V]
   float *part;                // [K][blocks][2][D]: sums of runs that cross the borders of a block
   long long ld, T;
   int V, D, K;
   int blk;                    // sorted positions of a block, a multiple of 32
   int blocks, slices;         // blocks of a replica; column slices of a row
-  long long sum_ctas;         // CTAs of the launch that sum; the ones after them write rows of zeros
   float scale;
   int accumulate;
 };
 
-template <typename G, int VEC>
-__device__ __forceinline__ void write_row(const GradArgs &a, G *p, float (&x)[VEC]) {
-  if (a.accumulate) {
-    float old[VEC];
-    load<G, VEC>(p, old);
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = fmaf(a.scale, x[i], old[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < VEC; ++i) x[i] = __fmul_rn(a.scale, x[i]);
-  }
-  store<G, VEC>(p, x);
-}
-
 constexpr int kSliceCols = 256;  // columns that a warp carries: 8 per lane
-constexpr int kSumWarps = 4, kAhead = 4, kZeroRows = 32;
+constexpr int kSumWarps = 4, kAhead = 8;
 
-// A warp walks one block of the sorted tokens over one slice of columns, kAhead rows of dy in flight, and ends a sum
-// wherever the token changes.  A run inside the block goes straight to the gradient; one that crosses a border leaves
-// its sum in `part`: slot 0 when it began in an earlier block, slot 1 when it begins here and goes on.
-template <typename Y, typename G, int VEC>
-__device__ void sum_block(const GradArgs &a, long long task) {
+// A warp walks one block of the sorted tokens over one slice of columns, kAhead rows of dy in flight (and the rows of the
+// gradient that they are added to), and ends a sum wherever the token changes.  A run inside the block goes straight to
+// the gradient; one that crosses a border leaves its sum in `part`: slot 0 when it began in an earlier block, slot 1 when it
+// begins here and goes on.
+template <typename Y, typename G, int VEC, bool ADD>
+__device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   constexpr int NV = 8 / VEC;
   const int lane = threadIdx.x & 31;
   const int s = (int)(task % a.slices);
@@ -281,53 +321,70 @@ __device__ void sum_block(const GradArgs &a, long long task) {
   const long long k = kb / a.blocks;
   const uint32_t none = (uint32_t)a.V;
   const uint32_t *key = a.key + k * a.T, *pos = a.pos + k * a.T;
+  const long long e0 = (long long)b * a.blk, e1 = min(a.T, e0 + a.blk);
+  const uint32_t first = key[e0], prev = e0 ? key[e0 - 1] : none, next = e1 < a.T ? key[e1] : none;
+  if (first == none) return;
+  const int c0 = s * kSliceCols + lane * VEC;
+  int col[NV];  // this lane's columns; the ones beyond D are read at column 0 and not written
+#pragma unroll
+  for (int u = 0; u < NV; ++u) col[u] = c0 + u * 32 * VEC < a.D ? c0 + u * 32 * VEC : -1;
   const Y *dy = static_cast<const Y *>(a.dy) + k * a.T * a.D;
   G *grad = static_cast<G *>(a.grad) + k * a.ld;
   float *part = a.part + (k * a.blocks + b) * 2 * a.D;
-  const long long e0 = (long long)b * a.blk, e1 = min(a.T, e0 + a.blk);
-  if (key[e0] == none) return;
-  const uint32_t prev = e0 ? key[e0 - 1] : none, next = e1 < a.T ? key[e1] : none;
-  const int c0 = s * kSliceCols + lane * VEC;
-  bool col[NV];
-#pragma unroll
-  for (int u = 0; u < NV; ++u) col[u] = c0 + u * 32 * VEC < a.D;
 
   float acc[NV][VEC] = {};
-  bool head = prev == key[e0];  // the first run of the block began earlier
+  bool head = prev == first;  // the first run of the block began earlier
   for (long long e = e0; e < e1; e += 32) {
     const int n = (int)min(32LL, e1 - e);
     const uint32_t kl = lane < n ? key[e + lane] : none, pl = lane < n ? pos[e + lane] : 0;
-    uint32_t after = e + 32 < e1 ? key[e + 32] : none;  // the key that follows lane 31 inside the block
+    uint32_t follow = __shfl_down_sync(0xffffffffu, kl, 1);
+    if (lane == 31) follow = e + 32 < e1 ? key[e + 32] : none;
+    const bool last = e + lane == e1 - 1;
+    // what an entry does when it has been added: 0 nothing, 1 its run ends in the block, 2 its run goes on in the next one
+    const int what = kl == none || (!last && follow == kl) ? 0 : last && next == kl ? 2 : 1;
     for (int j0 = 0; j0 < n; j0 += kAhead) {
-      float x[kAhead][NV][VEC];
+      if (__shfl_sync(0xffffffffu, kl, j0) == none) return;  // only tokens outside the table follow
+      Raw<Y, VEC> x[kAhead][NV];
+      Raw<G, VEC> old[ADD ? kAhead : 1][NV];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
-        const uint32_t kj = __shfl_sync(0xffffffffu, kl, j0 + j), pj = __shfl_sync(0xffffffffu, pl, j0 + j);
-        const Y *row = dy + (long long)pj * a.D + c0;
+        const Y *row = dy + (long long)__shfl_sync(0xffffffffu, pl, j0 + j) * a.D;  // row 0 past the end
 #pragma unroll
-        for (int u = 0; u < NV; ++u)
-          if (kj != none && col[u]) load<Y, VEC>(row + u * 32 * VEC, x[j][u]);
+        for (int u = 0; u < NV; ++u) x[j][u].load(row + max(col[u], 0));
+        if constexpr (ADD) {
+          const uint32_t kj = __shfl_sync(0xffffffffu, kl, j0 + j);
+          if (__shfl_sync(0xffffffffu, what, j0 + j) == 1)
+#pragma unroll
+            for (int u = 0; u < NV; ++u) old[j][u].load(grad + (long long)kj * a.D + max(col[u], 0));
+        }
       }
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         const uint32_t kj = __shfl_sync(0xffffffffu, kl, j0 + j);
-        const uint32_t kn = __shfl_sync(0xffffffffu, kl, (j0 + j + 1) & 31);
-        if (kj == none) continue;  // also the lanes past the end
+        const int wj = __shfl_sync(0xffffffffu, what, j0 + j);
+        if (kj != none) {
 #pragma unroll
-        for (int u = 0; u < NV; ++u)
+          for (int u = 0; u < NV; ++u) {
+            float v[VEC];
+            x[j][u].widen(v);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) acc[u][i] = __fadd_rn(acc[u][i], x[j][u][i]);
-        const bool last = e + j0 + j == e1 - 1;
-        const uint32_t follows = last ? none : (j0 + j == 31 ? after : kn);
-        if (follows == kj) continue;
-        const bool tail = last && next == kj;
+            for (int i = 0; i < VEC; ++i) acc[u][i] = __fadd_rn(acc[u][i], v[i]);
+          }
+        }
+        if (!wj) continue;
 #pragma unroll
         for (int u = 0; u < NV; ++u) {
-          if (!col[u]) continue;
-          const int c = c0 + u * 32 * VEC;
-          if (head) store<float, VEC>(part + c, acc[u]);
-          else if (tail) store<float, VEC>(part + a.D + c, acc[u]);
-          else write_row<G, VEC>(a, grad + (long long)kj * a.D + c, acc[u]);
+          if (col[u] >= 0) {
+            if (head || wj == 2) {
+              store<float, VEC>(part + (head ? 0 : a.D) + col[u], acc[u]);
+            } else {
+              float v[VEC], o[VEC] = {};
+              if constexpr (ADD) old[j][u].widen(o);
+#pragma unroll
+              for (int i = 0; i < VEC; ++i) v[i] = ADD ? fmaf(a.scale, acc[u][i], o[i]) : __fmul_rn(a.scale, acc[u][i]);
+              store<G, VEC>(grad + (long long)kj * a.D + col[u], v);
+            }
+          }
 #pragma unroll
           for (int i = 0; i < VEC; ++i) acc[u][i] = 0.f;
         }
@@ -337,68 +394,116 @@ __device__ void sum_block(const GradArgs &a, long long task) {
   }
 }
 
-template <typename Y, typename G, int VEC>
+template <typename Y, typename G, int VEC, bool ADD>
 __global__ void __launch_bounds__(kSumWarps * 32) k_embed_sum(const GradArgs a) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (blockIdx.x < a.sum_ctas) {
-    const long long task = (long long)blockIdx.x * kSumWarps + warp;
-    if (task < (long long)a.K * a.blocks * a.slices) sum_block<Y, G, VEC>(a, task);
-    return;
-  }
-  // rows that no token selects become zero
-  const long long z = blockIdx.x - a.sum_ctas, per = (a.V + kZeroRows - 1) / kZeroRows;
-  const long long k = z / per;
-  const int v0 = (int)(z % per) * kZeroRows;
-  const float zero[VEC] = {};
-  for (int v = v0 + warp; v < min(a.V, v0 + kZeroRows); v += kSumWarps) {
-    if (a.met[k * a.V + v]) continue;
-    G *row = static_cast<G *>(a.grad) + k * a.ld + (long long)v * a.D;
-    for (int c = lane * VEC; c < a.D; c += 32 * VEC) store<G, VEC>(row + c, zero);
-  }
+  asm volatile("griddepcontrol.launch_dependents;");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const long long task = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
+  if (task < (long long)a.K * a.blocks * a.slices) sum_block<Y, G, VEC, ADD>(a, task);
 }
 
-// The runs that cross blocks: one CTA for each block in which such a run begins, and 128 columns.  Its warps take every
-// eighth partial sum, the eight sums are added in the order of the warps.
-constexpr int kJoinWarps = 8, kJoinCols = 128;
+// The runs that cross blocks.  A run that spans few blocks is joined by one CTA, a thread for each column; one that spans
+// more than kLong of them by the CTAs of a second kind, one for 128 columns of a replica, whose warps share the blocks.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinCols = 128, kLong = 16;
+
+struct Run {
+  uint32_t v;   // the row, or V where no run that crosses into the next block begins in this one
+  bool lengthy; // it reaches beyond the kLong blocks after this one
+};
+
+__device__ __forceinline__ Run crossing(const GradArgs &a, const uint32_t *key, int b) {
+  const long long e0 = (long long)b * a.blk, e1 = e0 + a.blk, far = e1 + (long long)kLong * a.blk;
+  Run r{(uint32_t)a.V, false};
+  if (e1 >= a.T) return r;
+  const uint32_t v = key[e1 - 1], next = key[e1], first = key[e0], prev = e0 ? key[e0 - 1] : (uint32_t)a.V;
+  const uint32_t away = far < a.T ? key[far] : (uint32_t)a.V;
+  if (v == (uint32_t)a.V || next != v || (first == v && prev == v)) return r;
+  r.v = v, r.lengthy = away == v;
+  return r;
+}
 
 template <typename G>
-__global__ void __launch_bounds__(kJoinWarps * 32) k_embed_join(const GradArgs a) {
+__device__ __forceinline__ void add_row(const GradArgs &a, G *p, float x) {
+  const float y = a.accumulate ? fmaf(a.scale, x, static_cast<float>(*p)) : __fmul_rn(a.scale, x);
+  if constexpr (sizeof(G) == 4) *p = y;
+  else *p = __float2bfloat16_rn(y);
+}
+
+template <typename G>
+__global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
   __shared__ float sums[kJoinWarps][kJoinCols];
-  const int b = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long k = blockIdx.z;
+  __shared__ int found[kJoinThreads];
+  __shared__ int n_found;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const long long k = blockIdx.y;
   const uint32_t *key = a.key + k * a.T;
-  const long long e0 = (long long)b * a.blk, e1 = e0 + a.blk;
-  if (e1 >= a.T) return;
-  const uint32_t v = key[e1 - 1];
-  if (v == (uint32_t)a.V || key[e1] != v || (key[e0] == v && e0 && key[e0 - 1] == v)) return;
-  int n = 1;  // blocks after this one whose first run is this run; b + n is looked at next
-  for (;; n += 32) {
-    const long long e = (long long)(b + n + lane) * a.blk;
-    const unsigned more = __ballot_sync(0xffffffffu, e < a.T && key[min(e, a.T - 1)] == v);
-    if (more != 0xffffffffu) {
-      n += __ffs(~more) - 1;
-      break;
+  G *grad = static_cast<G *>(a.grad) + k * a.ld;
+  const int short_ctas = a.blocks - 1;
+  // part i of a run that begins in block b: slot 1 of block b for i = 0, slot 0 of block b + i after it
+  auto parts = [&](int b) { return a.part + (k * a.blocks + b) * 2 * a.D; };
+  if (blockIdx.x < short_ctas) {
+    const int b = blockIdx.x;
+    const Run r = crossing(a, key, b);
+    if (r.v == (uint32_t)a.V || r.lengthy) return;
+    const long long e = (long long)(b + 1 + lane) * a.blk;  // kLong < 32 blocks after this one
+    const unsigned more = __ballot_sync(0xffffffffu, e < a.T && key[min(e, a.T - 1)] == r.v);
+    const int n = __ffs(~more);  // parts: one and those after it
+    const float *part = parts(b);
+    for (int c = tid; c < a.D; c += kJoinThreads) {
+      float x[kLong + 1];
+#pragma unroll
+      for (int i = 0; i <= kLong; ++i) x[i] = i < n ? __ldg(part + (i ? (long long)i * 2 * a.D : (long long)a.D) + c) : 0.f;
+#pragma unroll
+      for (int i = 1; i <= kLong; ++i) x[0] = __fadd_rn(x[0], x[i]);
+      add_row(a, grad + (long long)r.v * a.D + c, x[0]);
     }
+    return;
   }
-  const float *part = a.part + (k * a.blocks + b) * 2 * a.D;  // part 0: slot 1 of block b; part i: slot 0 of block b + i
-  const int c = blockIdx.y * kJoinCols + lane;
-  float acc[kJoinCols / 32] = {};
-#pragma unroll 4
-  for (int i = warp; i < n; i += kJoinWarps) {
-    const float *p = part + (i ? (long long)i * 2 * a.D : (long long)a.D);
+  const int c0 = (blockIdx.x - short_ctas) * kJoinCols;
+  for (int from = 0; from < short_ctas; from += kJoinThreads) {
+    if (tid == 0) n_found = 0;
+    __syncthreads();
+    if (from + tid < short_ctas && crossing(a, key, from + tid).lengthy) found[atomicAdd(&n_found, 1)] = from + tid;
+    __syncthreads();
+    for (int f = 0; f < n_found; ++f) {  // in any order: every run is a row of its own
+      const int b = found[f];
+      const uint32_t v = key[(long long)b * a.blk + a.blk - 1];
+      int lo = b + kLong + 1, hi = a.blocks;  // the last block whose first token is v: binary search, the tokens are sorted
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (key[(long long)mid * a.blk] == v) lo = mid;
+        else hi = mid;
+      }
+      const int n = lo - b + 1;
+      const float *part = parts(b);
+      float acc[kJoinCols / 32] = {};
+      for (int i0 = warp; i0 < n; i0 += 8 * kJoinWarps) {
+        float x[8][kJoinCols / 32];
 #pragma unroll
-    for (int u = 0; u < kJoinCols / 32; ++u)
-      if (c + 32 * u < a.D) acc[u] = __fadd_rn(acc[u], __ldg(p + c + 32 * u));
-  }
+        for (int j = 0; j < 8; ++j) {
+          const int i = i0 + j * kJoinWarps;
+          const float *p = part + (i ? (long long)i * 2 * a.D : (long long)a.D);
 #pragma unroll
-  for (int u = 0; u < kJoinCols / 32; ++u) sums[warp][lane + 32 * u] = acc[u];
-  __syncthreads();
-  const int cc = blockIdx.y * kJoinCols + threadIdx.x;
-  if (threadIdx.x < kJoinCols && cc < a.D) {
-    float x[1] = {0.f};
+          for (int u = 0; u < kJoinCols / 32; ++u) x[j][u] = i < n && c0 + lane + 32 * u < a.D ? __ldg(p + c0 + lane + 32 * u) : 0.f;
+        }
 #pragma unroll
-    for (int w = 0; w < kJoinWarps; ++w) x[0] = __fadd_rn(x[0], sums[w][threadIdx.x]);
-    write_row<G, 1>(a, static_cast<G *>(a.grad) + k * a.ld + (long long)v * a.D + cc, x);
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int u = 0; u < kJoinCols / 32; ++u) acc[u] = __fadd_rn(acc[u], x[j][u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kJoinCols / 32; ++u) sums[warp][lane + 32 * u] = acc[u];
+      __syncthreads();
+      if (tid < kJoinCols && c0 + tid < a.D) {
+        float x = sums[0][tid];
+#pragma unroll
+        for (int w = 1; w < kJoinWarps; ++w) x = __fadd_rn(x, sums[w][tid]);
+        add_row(a, grad + (long long)v * a.D + c0 + tid, x);
+      }
+      __syncthreads();
+    }
+    __syncthreads();
   }
 }
 
@@ -451,7 +556,7 @@ bool wide(const dasgd_embed_config &c, const void *array, const void *rows) {
 
 struct Plan {  // of the gradient's workspace
   int blk, blocks, slices, passes, radix_bits, cluster;
-  size_t key[2], pos[2], met, part, bytes;
+  size_t key[2], pos[2], part, bytes;
 };
 
 constexpr int kBlkMax = 128, kBlkMin = 32, kEnoughWarps = 4096;
@@ -480,7 +585,6 @@ Plan plan(const dasgd_embed_config &c) {
   };
   const size_t list = (size_t)c.K * c.T * 4;
   for (int i = 0; i < 2; ++i) p.key[i] = take(list), p.pos[i] = take(list);
-  p.met = take((size_t)c.K * c.V);
   p.part = take((size_t)c.K * most * 2 * c.D * 4);
   p.bytes = at;
   return p;
@@ -497,10 +601,26 @@ void launch_lookup(const dasgd_embed_config &c, LookupArgs a, bool vec, cudaStre
   else k_embed_lookup<W, O, 1><<<grid, kThreads, 0, s>>>(a);
 }
 
+// on the stream, after the kernel before it has ended, but set up while that runs
+template <typename F, typename... A>
+cudaError_t launch_after(F kernel, dim3 grid, int threads, cudaStream_t s, const A &...args) {
+  cudaLaunchConfig_t lc{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.gridDim = grid, lc.blockDim = dim3(threads), lc.stream = s, lc.attrs = attr, lc.numAttrs = 1;
+  return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
 template <typename Y, typename G>
-void launch_sum(const GradArgs &a, bool vec, long long ctas, cudaStream_t s) {
-  if (vec) k_embed_sum<Y, G, 8><<<(unsigned)ctas, kSumWarps * 32, 0, s>>>(a);
-  else k_embed_sum<Y, G, 1><<<(unsigned)ctas, kSumWarps * 32, 0, s>>>(a);
+cudaError_t launch_sum(const GradArgs &a, bool vec, long long ctas, cudaStream_t s) {
+  const dim3 grid((unsigned)ctas);
+  if (a.accumulate) {
+    if (vec) return launch_after(k_embed_sum<Y, G, 8, true>, grid, kSumWarps * 32, s, a);
+    return launch_after(k_embed_sum<Y, G, 1, true>, grid, kSumWarps * 32, s, a);
+  }
+  if (vec) return launch_after(k_embed_sum<Y, G, 8, false>, grid, kSumWarps * 32, s, a);
+  return launch_after(k_embed_sum<Y, G, 1, false>, grid, kSumWarps * 32, s, a);
 }
 
 }  // namespace
@@ -556,10 +676,9 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
     return bad("embed_gradient: needs a 256-byte aligned workspace of " + std::to_string(p.bytes) + " bytes");
   if (!aligned(grad_array, size_of(c.table_elem)) || !aligned(dy, size_of(c.rows_elem)) || !aligned(tokens, c.token_bits / 8))
     return bad("embed_gradient: buffers must be aligned to their elements");
-  const long long zero_ctas = c.accumulate ? 0 : (long long)c.K * ((c.V + kZeroRows - 1) / kZeroRows);
   const long long sum_ctas = ((long long)c.K * p.blocks * p.slices + kSumWarps - 1) / kSumWarps;
-  if (sum_ctas + zero_ctas > INT32_MAX || p.blocks > INT32_MAX / 2)
-    return dasgd_internal_fail(nullptr, DASGD_ERR_UNSUPPORTED, "embed_gradient: K*V or K*T*D too large for one launch");
+  if (sum_ctas > INT32_MAX || p.blocks > INT32_MAX / 2)
+    return dasgd_internal_fail(nullptr, DASGD_ERR_UNSUPPORTED, "embed_gradient: K*T*D too large for one launch");
   OnDevice dev(c.device);
   if (dev.e != cudaSuccess) return cuda_fail(dev.e, "embed_gradient");
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -571,10 +690,16 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
     so.key[i] = reinterpret_cast<uint32_t *>(ws + p.key[i]);
     so.pos[i] = reinterpret_cast<uint32_t *>(ws + p.pos[i]);
   }
-  so.met = reinterpret_cast<uint8_t *>(ws + p.met);
   so.T = c.T, so.V = c.V, so.token_bits = c.token_bits, so.passes = p.passes, so.radix_bits = p.radix_bits;
+  so.K = c.K, so.sorted = c.T ? c.K : 0;
+  char *grad = static_cast<char *>(grad_array) + c.offset * size_of(c.table_elem);
+  long long zero_ctas = 0;
+  if (!c.accumulate) {
+    so.grad = grad, so.grad_stride = c.ld * size_of(c.table_elem), so.grad_bytes = (long long)c.V * c.D * size_of(c.table_elem);
+    zero_ctas = std::min<long long>(kZeroCtas, c.K * ((so.grad_bytes + kZeroPiece - 1) / kZeroPiece));
+  }
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3((unsigned)(c.K * p.cluster));
+  lc.gridDim = dim3((unsigned)(so.sorted * p.cluster + (zero_ctas + p.cluster - 1) / p.cluster * p.cluster));
   lc.blockDim = dim3(kSortThreads);
   lc.stream = s;
   cudaLaunchAttribute attr[1];
@@ -583,24 +708,27 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   lc.attrs = attr, lc.numAttrs = 1;
   cudaError_t e = cudaLaunchKernelEx(&lc, k_sort_tokens, so);
   if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sort");
+  if (!c.T) return DASGD_OK;
 
   GradArgs a{};
   a.dy = dy;
-  a.grad = static_cast<char *>(grad_array) + c.offset * size_of(c.table_elem);
-  a.key = so.key[p.passes & 1], a.pos = so.pos[p.passes & 1], a.met = so.met;
+  a.grad = grad;
+  a.key = so.key[p.passes & 1], a.pos = so.pos[p.passes & 1];
   a.part = reinterpret_cast<float *>(ws + p.part);
   a.ld = c.ld, a.T = c.T, a.V = c.V, a.D = c.D, a.K = c.K, a.blk = p.blk, a.blocks = p.blocks, a.slices = p.slices;
-  a.sum_ctas = sum_ctas, a.scale = c.scale, a.accumulate = c.accumulate != 0;
+  a.scale = c.scale, a.accumulate = c.accumulate != 0;
   const bool vec = wide(c, grad_array, dy);
   const bool y32 = c.rows_elem == DASGD_ELEM_F32, g32 = c.table_elem == DASGD_ELEM_F32;
-  if (y32 && g32) launch_sum<float, float>(a, vec, sum_ctas + zero_ctas, s);
-  else if (y32) launch_sum<float, __nv_bfloat16>(a, vec, sum_ctas + zero_ctas, s);
-  else if (g32) launch_sum<__nv_bfloat16, float>(a, vec, sum_ctas + zero_ctas, s);
-  else launch_sum<__nv_bfloat16, __nv_bfloat16>(a, vec, sum_ctas + zero_ctas, s);
+  if (y32 && g32) e = launch_sum<float, float>(a, vec, sum_ctas, s);
+  else if (y32) e = launch_sum<float, __nv_bfloat16>(a, vec, sum_ctas, s);
+  else if (g32) e = launch_sum<__nv_bfloat16, float>(a, vec, sum_ctas, s);
+  else e = launch_sum<__nv_bfloat16, __nv_bfloat16>(a, vec, sum_ctas, s);
+  if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sums");
   if (p.blocks > 1) {
-    const dim3 grid((unsigned)(p.blocks - 1), (unsigned)((c.D + kJoinCols - 1) / kJoinCols), (unsigned)c.K);
-    if (g32) k_embed_join<float><<<grid, kJoinWarps * 32, 0, s>>>(a);
-    else k_embed_join<__nv_bfloat16><<<grid, kJoinWarps * 32, 0, s>>>(a);
+    const int lengthy = p.blocks > kLong + 1 ? (c.D + kJoinCols - 1) / kJoinCols : 0;
+    const dim3 grid((unsigned)(p.blocks - 1 + lengthy), (unsigned)c.K);
+    e = g32 ? launch_after(k_embed_join<float>, grid, kJoinThreads, s, a) : launch_after(k_embed_join<__nv_bfloat16>, grid, kJoinThreads, s, a);
+    if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: joining");
   }
   e = cudaGetLastError();
   return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "embed_gradient");
