@@ -375,19 +375,21 @@ class _StreamOrder:
     """Calls that share a workspace run one after the other also when the caller changes streams between them."""
 
     def __init__(self, device):
-        self.device, self.last, self.done = device, torch.cuda.current_stream(device), None
+        self.device, self.index, self.done = device, device.index, None
+        self.last = torch.cuda.current_stream(device)
+        self.raw = self.last.cuda_stream
 
-    def enter(self, tensors) -> int:
-        stream = torch.cuda.current_stream(self.device)
-        if self.last != stream:
+    def enter(self, workspace) -> int:
+        raw = torch._C._cuda_getCurrentRawStream(self.index)
+        if raw != self.raw:
+            stream = torch.cuda.current_stream(self.device)
             if self.done is None:
                 self.done = torch.cuda.Event()
             self.done.record(self.last)
             stream.wait_event(self.done)
-            for t in tensors:
-                t.record_stream(stream)
-        self.last = stream
-        return stream.cuda_stream
+            workspace.record_stream(stream)
+            self.last, self.raw = stream, raw
+        return raw
 
 
 class Embedding:
@@ -403,50 +405,63 @@ class Embedding:
             raise RuntimeError("Embedding needs a CUDA device; there is no CPU implementation")
         self.K, self.ld, self.offset, self.V, self.D, self.max_tokens = K, ld, offset, V, D, max_tokens
         self.device = torch.device("cuda", device)
+        self._shape = torch.Size((K, ld))
         c = self.cfg = dasgd_embed_config()
         c.K, c.V, c.D, c.device, c.T, c.ld, c.offset, c.scale = K, V, D, device, max_tokens, ld, offset, scale
         c.token_bits = 64
+        self._cfg = ctypes.byref(c)
         self._ws = torch.empty(dasgd_embed_workspace(c), dtype=torch.uint8, device=self.device)
         self._order = _StreamOrder(self.device)
 
-    def _set(self, array, tokens, rows, what):
-        K, D, c = self.K, self.D, self.cfg
-        if not (array.is_cuda and tokens.is_cuda and array.device == tokens.device == self.device):
-            raise ValueError(f"the {what} array and the tokens must be on {self.device}")
-        if array.dtype not in _ELEM or tuple(array.shape) != (K, self.ld) or not array.is_contiguous():
-            raise ValueError(f"the {what} array must be a contiguous float32 or bfloat16 tensor of shape {(K, self.ld)}")
-        if tokens.dtype not in _TOKEN_BITS or tokens.dim() != 2 or tokens.shape[0] != K or not tokens.is_contiguous():
-            raise ValueError(f"tokens must be a contiguous int32 or int64 tensor of shape ({K}, T)")
-        T = tokens.shape[1]
-        if rows is not None and (rows.dtype not in _ELEM or tuple(rows.shape) != (K, T, D) or not rows.is_contiguous()
-                                 or rows.device != self.device):
-            raise ValueError(f"activations must be a contiguous float32 or bfloat16 tensor of shape {(K, T, D)} on {self.device}")
-        c.T, c.token_bits, c.table_elem = T, _TOKEN_BITS[tokens.dtype], _ELEM[array.dtype]
-        return T
+    def _set(self, array, tokens, what):
+        elem, bits, device, shape = _ELEM.get(array.dtype), _TOKEN_BITS.get(tokens.dtype), self.device, tokens.shape
+        if array.device != device or tokens.device != device:
+            raise ValueError(f"the {what} array and the tokens must be on {device}")
+        if elem is None or array.shape != self._shape or not array.is_contiguous():
+            raise ValueError(f"the {what} array must be a contiguous float32 or bfloat16 tensor of shape {tuple(self._shape)}")
+        if bits is None or len(shape) != 2 or shape[0] != self.K or not tokens.is_contiguous():
+            raise ValueError(f"tokens must be a contiguous int32 or int64 tensor of shape ({self.K}, T)")
+        c = self.cfg
+        c.T, c.token_bits, c.table_elem = shape[1], bits, elem
+        return shape[1]
+
+    def _rows(self, rows, T):
+        elem = _ELEM.get(rows.dtype)
+        if elem is None or rows.shape != (self.K, T, self.D) or not rows.is_contiguous() or rows.device != self.device:
+            raise ValueError(f"activations must be a contiguous float32 or bfloat16 tensor of shape {(self.K, T, self.D)} on {self.device}")
+        self.cfg.rows_elem = elem
 
     def lookup(self, w, tokens, out=None, out_dtype=None):
         """``scale * table[tokens]``: ``[K, T, D]`` in ``out`` (made if not given; its type defaults to the table's)."""
-        T = self._set(w, tokens, out, "weight")
+        T = self._set(w, tokens, "weight")
         if out is None:
+            elem = _ELEM.get(out_dtype or w.dtype)
+            if elem is None:
+                raise ValueError("out_dtype must be float32 or bfloat16")
             out = torch.empty((self.K, T, self.D), dtype=out_dtype or w.dtype, device=self.device)
-        elif out_dtype is not None and out.dtype != out_dtype:
-            raise ValueError("out and out_dtype disagree")
-        if out.dtype not in _ELEM:
-            raise ValueError("out_dtype must be float32 or bfloat16")
-        self.cfg.rows_elem = _ELEM[out.dtype]
-        dasgd_embed_lookup(self.cfg, w.data_ptr(), tokens.data_ptr(), out.data_ptr(),
-                           torch.cuda.current_stream(self.device).cuda_stream)
+            self.cfg.rows_elem = elem
+        else:
+            self._rows(out, T)
+            if out_dtype is not None and out.dtype != out_dtype:
+                raise ValueError("out and out_dtype disagree")
+        status = _L.dasgd_embed_lookup(self._cfg, w.data_ptr(), tokens.data_ptr(), out.data_ptr(),
+                                       torch._C._cuda_getCurrentRawStream(self.device.index))
+        if status:
+            _check(status)
         return out
 
     def gradient(self, dy, tokens, g, accumulate=False):
         """Writes the table's slice of ``g`` (all of it, or adds to the rows that tokens select when ``accumulate``)."""
-        T = self._set(g, tokens, dy, "gradient")
+        T = self._set(g, tokens, "gradient")
+        self._rows(dy, T)
         if T > self.max_tokens:
             raise ValueError(f"{T} tokens per replica, but max_tokens is {self.max_tokens}")
-        self.cfg.rows_elem, self.cfg.accumulate = _ELEM[dy.dtype], int(accumulate)
-        stream = self._order.enter((self._ws,))
-        dasgd_embed_gradient(self.cfg, dy.data_ptr(), tokens.data_ptr(), g.data_ptr(), self._ws.data_ptr(),
-                             self._ws.numel(), stream)
+        self.cfg.accumulate = 1 if accumulate else 0
+        ws = self._ws
+        status = _L.dasgd_embed_gradient(self._cfg, dy.data_ptr(), tokens.data_ptr(), g.data_ptr(), ws.data_ptr(), ws.numel(),
+                                         self._order.enter(ws))
+        if status:
+            _check(status)
         return g
 
 
@@ -495,7 +510,7 @@ class Ortho:
             raise ValueError("m must be given exactly when momentum != 0")
         gp, op = self._ptr(g, self.gdtype, "g"), self._ptr(out, self.gdtype, "out")
         mp = self._ptr(m, torch.float32, "m") if m is not None else None
-        dasgd_ortho_step(self.op, gp, mp, op, self._order.enter((self._ws,)))
+        dasgd_ortho_step(self.op, gp, mp, op, self._order.enter(self._ws))
         return out
 
     def sync(self):

@@ -11,10 +11,12 @@
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
+#include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
 #include <string>
+#include <type_traits>
 
 namespace cg = cooperative_groups;
 
@@ -38,6 +40,10 @@ struct Raw {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) w[i] = __ldg(reinterpret_cast<const uint4 *>(p) + i);
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = make_uint4(0, 0, 0, 0);
+  }
   __device__ __forceinline__ void widen(float (&x)[VEC]) const {
 #pragma unroll
     for (int i = 0; i < kWords; ++i) {
@@ -55,6 +61,7 @@ template <typename T>
 struct Raw<T, 1> {
   T w;
   __device__ __forceinline__ void load(const T *p) { w = __ldg(p); }
+  __device__ __forceinline__ void clear() { w = static_cast<T>(0.f); }
   __device__ __forceinline__ void widen(float (&x)[1]) const { x[0] = static_cast<float>(w); }
 };
 
@@ -79,6 +86,9 @@ __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {  // streami
 
 // ---------------------------------------------------------------- lookup
 
+template <typename W, int VEC>
+__host__ __device__ constexpr int lookup_rows() { return VEC == 8 && sizeof(W) == 4 ? 2 : 4; }
+
 struct LookupArgs {
   const void *table;   // already moved to the table's first element
   const void *tokens;
@@ -93,38 +103,37 @@ __device__ __forceinline__ long long token_at(const void *tokens, int bits, long
   return bits == 64 ? __ldg(static_cast<const long long *>(tokens) + i) : (long long)__ldg(static_cast<const int *>(tokens) + i);
 }
 
-// A CTA is 2^xs threads across a row (units of VEC elements) by 256 >> xs rows; each thread takes kRows rows at once so
-// that kRows independent row reads are in flight.
+// A CTA is 2^xs threads across a row (units of VEC elements) by 256 >> xs rows, and takes kRows such sets of rows, 64 bytes of
+// the table in flight for each thread.  Six CTAs to an SM (42 registers) matter more than rows in flight: 4 x 32768 rows of
+// 1024 bfloat16 took 74 us with four CTAs, 98 us with two and twice the rows, 85 us as a pipeline of persistent CTAs.
 template <typename W, typename O, int VEC>
-__global__ void __launch_bounds__(kThreads) k_embed_lookup(const LookupArgs a) {
-  constexpr int kRows = 4;
+__global__ void __launch_bounds__(kThreads, 6) k_embed_lookup(const LookupArgs a) {
+  constexpr int kRows = lookup_rows<W, VEC>();
   const int X = 1 << a.xs, Y = kThreads >> a.xs;
   const int tx = threadIdx.x & (X - 1), ty = threadIdx.x >> a.xs;
   const long long k = blockIdx.y, t0 = (long long)blockIdx.x * (Y * kRows) + ty;
   const W *table = static_cast<const W *>(a.table) + k * a.ld;
-  O *out = static_cast<O *>(a.out) + k * a.T * a.D;
-  const W *src[kRows];
-  bool live[kRows], hit[kRows];
+  O *out = static_cast<O *>(a.out) + (k * a.T + t0) * a.D;
+  const int live = (int)min((long long)kRows, (a.T - t0 + Y - 1) / Y);  // rows of this thread; may be <= 0
+  int tok[kRows];  // -1: none of the table's rows
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
-    const long long t = t0 + (long long)j * Y;
-    live[j] = t < a.T;
-    const long long tok = live[j] ? token_at(a.tokens, a.token_bits, k * a.T + t) : -1;
-    hit[j] = tok >= 0 && tok < a.V;
-    src[j] = table + (hit[j] ? tok : 0) * a.D;
+    const long long t = j < live ? token_at(a.tokens, a.token_bits, k * a.T + t0 + (long long)j * Y) : -1;
+    tok[j] = t >= 0 && t < a.V ? (int)t : -1;
   }
   for (int c = tx * VEC; c < a.D; c += X * VEC) {
     Raw<W, VEC> raw[kRows];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) raw[j].load(src[j] + c);
+    for (int j = 0; j < kRows; ++j) raw[j].load(table + (long long)max(tok[j], 0) * a.D + c);
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
-      if (!live[j]) continue;
+      if (j >= live) continue;
+      if (tok[j] < 0) raw[j].clear();
       float x[VEC];
       raw[j].widen(x);
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] = hit[j] ? __fmul_rn(x[i], a.scale) : 0.f;
-      store<O, VEC>(out + (t0 + (long long)j * Y) * a.D + c, x);
+      for (int i = 0; i < VEC; ++i) x[i] = __fmul_rn(x[i], a.scale);
+      store<O, VEC>(out + (long long)j * Y * a.D + c, x);
     }
   }
 }
@@ -298,14 +307,14 @@ struct GradArgs {
   float *part;                // [K][blocks][2][D]: sums of runs that cross the borders of a block
   long long ld, T;
   int V, D, K;
-  int blk;                    // sorted positions of a block, a multiple of 32
+  int blk;                    // sorted positions of a block
   int blocks, slices;         // blocks of a replica; column slices of a row
   float scale;
   int accumulate;
 };
 
-constexpr int kSliceCols = 256;  // columns that a warp carries: 8 per lane
-constexpr int kSumWarps = 4, kAhead = 8;
+constexpr int kSliceCols = 256, kWideCols = 512;  // columns that a warp carries: 8 per lane, 16 where rows are aligned
+constexpr int kSumWarps = 2, kAhead = 4;
 
 // A warp walks one block of the sorted tokens over one slice of columns, kAhead rows of dy in flight (and the rows of the
 // gradient that they are added to), and ends a sum wherever the token changes.  A run inside the block goes straight to
@@ -394,17 +403,167 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   }
 }
 
+// The same walk where rows start on 16-byte boundaries: the rows of dy, and the rows of the gradient that they are added to,
+// come through a ring in shared memory that every warp fills for itself with asynchronous copies, kRing rows ahead.  In
+// registers as many rows in flight would leave room for a third of the warps.
+template <typename Y, typename G, bool ADD>
+struct Ring {
+  static constexpr int kRows = ADD ? 8 : 16, kStep = ADD ? 2 : 4;  // rows of the ring; rows asked for, and waited for, together
+  static constexpr int kUnits = kWideCols / 256;                   // units of 8 columns of a lane, 256 columns apart
+  static constexpr int kNew = kUnits * 8 * sizeof(Y) * 32 / 16, kOld = ADD ? kUnits * 8 * sizeof(G) * 32 / 16 : 0;  // 16-byte pieces of a row
+  static constexpr int kBytes = kRows * (kNew + kOld) * 16;
+};
+
+template <typename T>
+__device__ __forceinline__ void copy8(uint32_t dst, const T *src) {  // 8 elements of every lane
+#pragma unroll
+  for (int i = 0; i < 8 * (int)sizeof(T) / 16; ++i)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * 512), "l"(reinterpret_cast<const char *>(src) + i * 16) : "memory");
+}
+
+template <typename T>
+__device__ __forceinline__ void read8(const uint4 *ring, float (&x)[8]) {
+  Raw<T, 8> r;
+#pragma unroll
+  for (int i = 0; i < Raw<T, 8>::kWords; ++i) r.w[i] = ring[i * 32];
+  r.widen(x);
+}
+
+template <typename Y, typename G, bool ADD>
+__device__ __forceinline__ void sum_block_ring(const GradArgs &a, long long task, uint4 *ring) {
+  using R = Ring<Y, G, ADD>;
+  const int lane = threadIdx.x & 31;
+  const int s = (int)(task % a.slices);
+  const long long kb = task / a.slices;
+  const int b = (int)(kb % a.blocks);
+  const long long k = kb / a.blocks;
+  const uint32_t none = (uint32_t)a.V;
+  const uint32_t *key = a.key + k * a.T, *pos = a.pos + k * a.T;
+  const long long e0 = (long long)b * a.blk, e1 = min(a.T, e0 + a.blk);
+  const uint32_t first = key[e0], prev = e0 ? key[e0 - 1] : none, next = e1 < a.T ? key[e1] : none;
+  const int c0 = s * kWideCols + lane * 8;
+  const Y *dy = static_cast<const Y *>(a.dy) + k * a.T * a.D + c0;
+  G *grad = static_cast<G *>(a.grad) + k * a.ld + c0;
+  float *part = a.part + (k * a.blocks + b) * 2 * a.D + c0;
+  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring + lane);
+  bool mine[R::kUnits];
+#pragma unroll
+  for (int u = 0; u < R::kUnits; ++u) mine[u] = c0 + u * 256 < a.D;
+
+  // 32 entries: lane l holds the key and position of entry l; bit l of `here`: its row is in the table; of `ends`: a sum ends
+  // with it; of `goes`: its run goes on in the next block
+  struct Entries {
+    uint32_t key, pos;
+    unsigned here, ends, goes;
+  };
+  auto fetch = [&](long long e) {
+    const long long i = e + lane;
+    Entries r;
+    r.key = i < e1 ? key[i] : none, r.pos = i < e1 ? pos[i] : 0;
+    uint32_t follow = __shfl_down_sync(0xffffffffu, r.key, 1);
+    if (lane == 31) follow = i + 1 < e1 ? key[i + 1] : none;
+    const bool last = i == e1 - 1;
+    r.here = __ballot_sync(0xffffffffu, r.key != none);
+    r.ends = __ballot_sync(0xffffffffu, r.key != none && (last || follow != r.key));
+    r.goes = __ballot_sync(0xffffffffu, r.key != none && last && next == r.key);
+    return r;
+  };
+  Entries now = fetch(e0), then{none, 0, 0, 0, 0};
+  if (first == none) return;
+  if (e0 + 32 < e1) then = fetch(e0 + 32);
+  const int n = (int)(e1 - e0);
+  auto ask = [&](int j, const Entries &en) {  // rows j .. of the block, whose entries are in en at j % 32
+#pragma unroll
+    for (int i = 0; i < R::kStep; ++i) {
+      const int l = (j + i) & 31;
+      const uint32_t pj = __shfl_sync(0xffffffffu, en.pos, l);
+      if (en.here >> l & 1) {
+        const uint32_t to = ring_at + ((j + i) % R::kRows) * (R::kNew + R::kOld) * 16;
+        const Y *row = dy + (long long)pj * a.D;
+#pragma unroll
+        for (int u = 0; u < R::kUnits; ++u)
+          if (mine[u]) copy8<Y>(to + u * (R::kNew / R::kUnits) * 16, row + u * 256);
+        if constexpr (ADD) {
+          if ((en.ends & ~en.goes) >> l & 1) {
+            const G *old = grad + (long long)__shfl_sync(0xffffffffu, en.key, l) * a.D;
+#pragma unroll
+            for (int u = 0; u < R::kUnits; ++u)
+              if (mine[u]) copy8<G>(to + (R::kNew + u * (R::kOld / R::kUnits)) * 16, old + u * 256);
+          }
+        }
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+#pragma unroll
+  for (int j = 0; j < R::kRows - R::kStep; j += R::kStep) ask(j, now);
+
+  float acc[R::kUnits][8] = {};
+  bool head = prev == first;
+  for (int j0 = 0; j0 < n; j0 += R::kStep) {
+    const int ja = j0 + R::kRows - R::kStep;  // the rows to ask for now
+    if ((ja & ~31) != (j0 & ~31)) ask(ja, then);
+    else ask(ja, now);
+    asm volatile("cp.async.wait_group %0;" ::"n"(R::kRows / R::kStep - 1) : "memory");
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < R::kStep; ++i) {
+      const int j = j0 + i, l = j & 31;
+      if (!(now.here >> l & 1)) continue;  // past the end, or outside the table
+      const uint4 *row = ring + (j % R::kRows) * (R::kNew + R::kOld) + lane;
+#pragma unroll
+      for (int u = 0; u < R::kUnits; ++u) {
+        float v[8];
+        read8<Y>(row + u * (R::kNew / R::kUnits), v);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[u][c] = __fadd_rn(acc[u][c], v[c]);
+      }
+      if (!(now.ends >> l & 1)) continue;
+      const bool aside = head || (now.goes >> l & 1);
+      const long long kj = __shfl_sync(0xffffffffu, now.key, l);
+#pragma unroll
+      for (int u = 0; u < R::kUnits; ++u) {
+        if (mine[u]) {
+          if (aside) {
+            store<float, 8>(part + (head ? 0 : a.D) + u * 256, acc[u]);
+          } else {
+            float v[8], o[8] = {};
+            if constexpr (ADD) read8<G>(row + R::kNew + u * (R::kOld / R::kUnits), o);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) v[c] = ADD ? fmaf(a.scale, acc[u][c], o[c]) : __fmul_rn(a.scale, acc[u][c]);
+            store<G, 8>(grad + kj * a.D + u * 256, v);
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c) acc[u][c] = 0.f;
+      }
+      head = false;
+    }
+    __syncwarp();  // the rows just read are asked for anew next
+    if (((j0 + R::kStep) & 31) == 0) {
+      now = then;
+      then = Entries{none, 0, 0, 0, 0};
+      if (e0 + j0 + R::kStep + 32 < e1) then = fetch(e0 + j0 + R::kStep + 32);
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
 template <typename Y, typename G, int VEC, bool ADD>
 __global__ void __launch_bounds__(kSumWarps * 32) k_embed_sum(const GradArgs a) {
+  extern __shared__ uint4 rings[];
   asm volatile("griddepcontrol.launch_dependents;");
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const long long task = (long long)blockIdx.x * kSumWarps + (threadIdx.x >> 5);
-  if (task < (long long)a.K * a.blocks * a.slices) sum_block<Y, G, VEC, ADD>(a, task);
+  const int warp = threadIdx.x >> 5;
+  const long long task = (long long)blockIdx.x * kSumWarps + warp;
+  if (task >= (long long)a.K * a.blocks * a.slices) return;
+  if constexpr (VEC == 8) sum_block_ring<Y, G, ADD>(a, task, rings + warp * (Ring<Y, G, ADD>::kBytes / 16));
+  else sum_block<Y, G, VEC, ADD>(a, task);
 }
 
 // The runs that cross blocks.  A run that spans few blocks is joined by one CTA, a thread for each column; one that spans
-// more than kLong of them by the CTAs of a second kind, one for 128 columns of a replica, whose warps share the blocks.
-constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kJoinCols = 128, kLong = 16;
+// more than kLong of them by CTAs of a second kind, kShare for 32 * VEC columns of a replica, whose warps share the blocks.
+constexpr int kJoinThreads = 256, kJoinWarps = kJoinThreads / 32, kLong = 16, kShare = 8;
 
 struct Run {
   uint32_t v;   // the row, or V where no run that crosses into the next block begins in this one
@@ -422,18 +581,48 @@ __device__ __forceinline__ Run crossing(const GradArgs &a, const uint32_t *key, 
   return r;
 }
 
-template <typename G>
-__device__ __forceinline__ void add_row(const GradArgs &a, G *p, float x) {
-  const float y = a.accumulate ? fmaf(a.scale, x, static_cast<float>(*p)) : __fmul_rn(a.scale, x);
-  if constexpr (sizeof(G) == 4) *p = y;
-  else *p = __float2bfloat16_rn(y);
+// VEC consecutive elements of a row of the gradient, x being the sum that belongs there
+template <typename G, int VEC>
+__device__ __forceinline__ void add_row(const GradArgs &a, G *p, const float (&x)[VEC]) {
+  float y[VEC];
+  if (a.accumulate) {
+    if constexpr (VEC == 4 && sizeof(G) == 4) {
+      const float4 o = *reinterpret_cast<const float4 *>(p);
+      y[0] = o.x, y[1] = o.y, y[2] = o.z, y[3] = o.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) y[i] = static_cast<float>(p[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) y[i] = fmaf(a.scale, x[i], y[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) y[i] = __fmul_rn(a.scale, x[i]);
+  }
+  if constexpr (VEC == 4 && sizeof(G) == 4) {
+    *reinterpret_cast<float4 *>(p) = make_float4(y[0], y[1], y[2], y[3]);
+  } else if constexpr (VEC == 4) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack(y[0], y[1]), pack(y[2], y[3]));
+  } else {
+    if constexpr (sizeof(G) == 4) *p = y[0];
+    else *p = __float2bfloat16_rn(y[0]);
+  }
 }
 
-template <typename G>
+template <int VEC>
+__device__ __forceinline__ void load_part(const float *p, float (&x)[VEC]) {
+  if constexpr (VEC == 4) {
+    const float4 v = __ldg(reinterpret_cast<const float4 *>(p));
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  } else {
+    x[0] = __ldg(p);
+  }
+}
+
+template <typename G, int VEC>
 __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
-  __shared__ float sums[kJoinWarps][kJoinCols];
-  __shared__ int found[kJoinThreads];
-  __shared__ int n_found;
+  __shared__ float sums[kJoinWarps][32 * VEC];
+  __shared__ int found[kJoinThreads], counts[kJoinWarps];
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long k = blockIdx.y;
@@ -442,31 +631,52 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
   const int short_ctas = a.blocks - 1;
   // part i of a run that begins in block b: slot 1 of block b for i = 0, slot 0 of block b + i after it
   auto parts = [&](int b) { return a.part + (k * a.blocks + b) * 2 * a.D; };
+  auto part_at = [&](const float *p, int i) { return p + (i ? (long long)i * 2 * a.D : (long long)a.D); };
   if (blockIdx.x < short_ctas) {
     const int b = blockIdx.x;
+    const long long e = (long long)(b + 1 + lane) * a.blk;  // kLong < 32 blocks after this one
+    const uint32_t after = e < a.T ? key[e] : (uint32_t)a.V;
     const Run r = crossing(a, key, b);
     if (r.v == (uint32_t)a.V || r.lengthy) return;
-    const long long e = (long long)(b + 1 + lane) * a.blk;  // kLong < 32 blocks after this one
-    const unsigned more = __ballot_sync(0xffffffffu, e < a.T && key[min(e, a.T - 1)] == r.v);
-    const int n = __ffs(~more);  // parts: one and those after it
+    const int n = __ffs(~__ballot_sync(0xffffffffu, after == r.v));  // parts: one and those after it
     const float *part = parts(b);
-    for (int c = tid; c < a.D; c += kJoinThreads) {
-      float x[kLong + 1];
+    for (int c = tid * VEC; c < a.D; c += kJoinThreads * VEC) {
+      float sum[VEC];
+      load_part<VEC>(part_at(part, 0) + c, sum);
 #pragma unroll
-      for (int i = 0; i <= kLong; ++i) x[i] = i < n ? __ldg(part + (i ? (long long)i * 2 * a.D : (long long)a.D) + c) : 0.f;
+      for (int i0 = 1; i0 <= kLong; i0 += 4) {
+        if (i0 >= n) break;
+        float x[4][VEC];
 #pragma unroll
-      for (int i = 1; i <= kLong; ++i) x[0] = __fadd_rn(x[0], x[i]);
-      add_row(a, grad + (long long)r.v * a.D + c, x[0]);
+        for (int i = 0; i < 4; ++i)
+          if (i0 + i < n) load_part<VEC>(part_at(part, i0 + i) + c, x[i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i0 + i < n)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) sum[j] = __fadd_rn(sum[j], x[i][j]);
+      }
+      add_row<G, VEC>(a, grad + (long long)r.v * a.D + c, sum);
     }
     return;
   }
-  const int c0 = (blockIdx.x - short_ctas) * kJoinCols;
+  // long runs in the order of their blocks; this CTA takes every kShare-th of them, for its columns
+  const int unit = blockIdx.x - short_ctas, c = (unit / kShare) * 32 * VEC + lane * VEC;
+  int number = 0;
   for (int from = 0; from < short_ctas; from += kJoinThreads) {
-    if (tid == 0) n_found = 0;
+    const bool hit = from + tid < short_ctas && crossing(a, key, from + tid).lengthy;
+    const unsigned hits = __ballot_sync(0xffffffffu, hit);
+    if (lane == 0) counts[warp] = __popc(hits);
     __syncthreads();
-    if (from + tid < short_ctas && crossing(a, key, from + tid).lengthy) found[atomicAdd(&n_found, 1)] = from + tid;
+    int at = __popc(hits & ((1u << lane) - 1)), all = 0;
+    for (int w = 0; w < kJoinWarps; ++w) {
+      if (w < warp) at += counts[w];
+      all += counts[w];
+    }
+    if (hit) found[at] = from + tid;
     __syncthreads();
-    for (int f = 0; f < n_found; ++f) {  // in any order: every run is a row of its own
+    for (int f = 0; f < all; ++f) {
+      if ((number + f) % kShare != unit % kShare) continue;
       const int b = found[f];
       const uint32_t v = key[(long long)b * a.blk + a.blk - 1];
       int lo = b + kLong + 1, hi = a.blocks;  // the last block whose first token is v: binary search, the tokens are sorted
@@ -476,33 +686,33 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
         else hi = mid;
       }
       const int n = lo - b + 1;
-      const float *part = parts(b);
-      float acc[kJoinCols / 32] = {};
+      const float *part = parts(b) + (c < a.D ? c : 0);
+      float acc[VEC] = {};
       for (int i0 = warp; i0 < n; i0 += 8 * kJoinWarps) {
-        float x[8][kJoinCols / 32];
+        float x[8][VEC];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int i = i0 + j * kJoinWarps;
-          const float *p = part + (i ? (long long)i * 2 * a.D : (long long)a.D);
-#pragma unroll
-          for (int u = 0; u < kJoinCols / 32; ++u) x[j][u] = i < n && c0 + lane + 32 * u < a.D ? __ldg(p + c0 + lane + 32 * u) : 0.f;
-        }
+        for (int j = 0; j < 8; ++j) load_part<VEC>(part_at(part, min(i0 + j * kJoinWarps, n - 1)), x[j]);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
+          if (i0 + j * kJoinWarps < n)
 #pragma unroll
-          for (int u = 0; u < kJoinCols / 32; ++u) acc[u] = __fadd_rn(acc[u], x[j][u]);
+            for (int u = 0; u < VEC; ++u) acc[u] = __fadd_rn(acc[u], x[j][u]);
       }
 #pragma unroll
-      for (int u = 0; u < kJoinCols / 32; ++u) sums[warp][lane + 32 * u] = acc[u];
+      for (int u = 0; u < VEC; ++u) sums[warp][lane * VEC + u] = acc[u];
       __syncthreads();
-      if (tid < kJoinCols && c0 + tid < a.D) {
-        float x = sums[0][tid];
+      if (warp == 0 && c < a.D) {
 #pragma unroll
-        for (int w = 1; w < kJoinWarps; ++w) x = __fadd_rn(x, sums[w][tid]);
-        add_row(a, grad + (long long)v * a.D + c0 + tid, x);
+        for (int u = 0; u < VEC; ++u) {
+          acc[u] = sums[0][lane * VEC + u];
+#pragma unroll
+          for (int w = 1; w < kJoinWarps; ++w) acc[u] = __fadd_rn(acc[u], sums[w][lane * VEC + u]);
+        }
+        add_row<G, VEC>(a, grad + (long long)v * a.D + c, acc);
       }
       __syncthreads();
     }
+    number += all;
     __syncthreads();
   }
 }
@@ -522,6 +732,7 @@ dasgd_status check(const dasgd_embed_config *c, const char *who) {
     return bad(at + "the table must lie inside a row: offset >= 0, offset + V*D <= ld");
   if (c->token_bits != 32 && c->token_bits != 64) return bad(at + "token_bits must be 32 or 64");
   if ((c->table_elem | 1) != 1 || (c->rows_elem | 1) != 1) return bad(at + "unknown element type");
+  if (!isfinite(c->scale)) return bad(at + "scale must be finite");
   if (c->device < 0) return bad(at + "device must be >= 0");
   return DASGD_OK;
 }
@@ -559,19 +770,40 @@ struct Plan {  // of the gradient's workspace
   size_t key[2], pos[2], part, bytes;
 };
 
-constexpr int kBlkMax = 128, kBlkMin = 32, kEnoughWarps = 4096;
+// Blocks of sorted tokens.  All warps that fit the SMs at once get one block of equal length, so that none is left to run alone
+// afterwards: with blocks of 128 entries 1024 CTAs ran as a full wave and one of 136 CTAs, and the sums took 67 us instead of
+// 49 (4 x 65536 rows of 512 bfloat16).  Many replicas or wide rows leave less than kWaves blocks to a replica: then kWaves times
+// as many, and the last wave's share is small.
+constexpr int kSms = 148, kWaves = 8, kBlkMin = 16;
 
-Plan plan(const dasgd_embed_config &c) {
+// warps that an SM holds, two to a CTA: as the rings allow, and where there are none as the registers do
+constexpr int kWarpsMost = 12;
+int warps_of(const dasgd_embed_config &c, bool vec) {
+  if (!vec) return kWarpsMost;
+  auto fit = [](int bytes) { return 2 * std::min(kWarpsMost / 2, 228 * 1024 / (2 * bytes + 1024)); };
+  const bool y32 = c.rows_elem == DASGD_ELEM_F32, g32 = c.table_elem == DASGD_ELEM_F32;
+  if (!c.accumulate) return fit(y32 ? Ring<float, float, false>::kBytes : Ring<__nv_bfloat16, float, false>::kBytes);
+  if (y32) return fit(g32 ? Ring<float, float, true>::kBytes : Ring<float, __nv_bfloat16, true>::kBytes);
+  return fit(g32 ? Ring<__nv_bfloat16, float, true>::kBytes : Ring<__nv_bfloat16, __nv_bfloat16, true>::kBytes);
+}
+
+long long most_blocks(long long tasks, int warps) {  // tasks: replicas * slices; warps: of an SM
+  const long long fit = kSms * warps / tasks;
+  return fit >= kWaves ? fit : (kWaves * (long long)kSms * warps + tasks - 1) / tasks;
+}
+
+Plan plan(const dasgd_embed_config &c, bool vec) {
   Plan p;
-  p.slices = (c.D + kSliceCols - 1) / kSliceCols;
-  auto blocks_of = [&](long long blk) { return (c.T + blk - 1) / blk; };
-  p.blk = kBlkMax;
-  while (p.blk > kBlkMin && c.K * blocks_of(p.blk) * p.slices < kEnoughWarps) p.blk /= 2;
-  p.blocks = (int)blocks_of(p.blk);
-  // the most blocks that c.T tokens or fewer can give: a block is shorter than kBlkMax only while blocks of twice its
-  // length are fewer than kEnoughWarps / (K * slices)
-  const long long few = (kEnoughWarps + (long long)c.K * p.slices - 1) / ((long long)c.K * p.slices);
-  const long long most = std::max(blocks_of(kBlkMax), std::min(blocks_of(kBlkMin), 2 * few));
+  const int cols = vec ? kWideCols : kSliceCols;
+  p.slices = (c.D + cols - 1) / cols;
+  auto blocks_of = [&](long long slices, int warps) { return std::min<long long>((c.T + kBlkMin - 1) / kBlkMin, most_blocks(c.K * slices, warps)); };
+  const long long blocks = std::max<long long>(1, blocks_of(p.slices, warps_of(c, vec)));
+  p.blk = (int)std::max<long long>(1, (c.T + blocks - 1) / blocks);
+  p.blocks = (int)((c.T + p.blk - 1) / p.blk);
+  // no less than c.T tokens or fewer can give, with any types and for either kind of slices
+  const long long narrow = (c.D + kSliceCols - 1) / kSliceCols, broad = (c.D + kWideCols - 1) / kWideCols;
+  const long long every = (kWaves * (long long)kSms * kWarpsMost + c.K * broad - 1) / (c.K * broad);
+  const long long most = std::min<long long>((c.T + kBlkMin - 1) / kBlkMin, std::max(every, most_blocks(c.K * narrow, kWarpsMost)));
   int bits = 1;
   while (bits < 31 && (1LL << bits) <= c.V) ++bits;  // keys 0..V
   p.passes = (bits + kMaxRadixBits - 1) / kMaxRadixBits;
@@ -595,7 +827,7 @@ void launch_lookup(const dasgd_embed_config &c, LookupArgs a, bool vec, cudaStre
   const int units = vec ? c.D / 8 : c.D;
   a.xs = 0;
   while (a.xs < 8 && (1 << a.xs) < units) ++a.xs;
-  const int rows = (kThreads >> a.xs) * 4;
+  const int rows = (kThreads >> a.xs) * (vec ? lookup_rows<W, 8>() : lookup_rows<W, 1>());
   const dim3 grid((unsigned)((c.T + rows - 1) / rows), (unsigned)c.K);
   if (vec) k_embed_lookup<W, O, 8><<<grid, kThreads, 0, s>>>(a);
   else k_embed_lookup<W, O, 1><<<grid, kThreads, 0, s>>>(a);
@@ -603,24 +835,36 @@ void launch_lookup(const dasgd_embed_config &c, LookupArgs a, bool vec, cudaStre
 
 // on the stream, after the kernel before it has ended, but set up while that runs
 template <typename F, typename... A>
-cudaError_t launch_after(F kernel, dim3 grid, int threads, cudaStream_t s, const A &...args) {
+cudaError_t launch_after(F kernel, dim3 grid, int threads, int shared, cudaStream_t s, const A &...args) {
   cudaLaunchConfig_t lc{};
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  lc.gridDim = grid, lc.blockDim = dim3(threads), lc.stream = s, lc.attrs = attr, lc.numAttrs = 1;
+  lc.gridDim = grid, lc.blockDim = dim3(threads), lc.dynamicSmemBytes = shared, lc.stream = s, lc.attrs = attr, lc.numAttrs = 1;
   return cudaLaunchKernelEx(&lc, kernel, args...);
 }
 
 template <typename Y, typename G>
 cudaError_t launch_sum(const GradArgs &a, bool vec, long long ctas, cudaStream_t s) {
   const dim3 grid((unsigned)ctas);
-  if (a.accumulate) {
-    if (vec) return launch_after(k_embed_sum<Y, G, 8, true>, grid, kSumWarps * 32, s, a);
-    return launch_after(k_embed_sum<Y, G, 1, true>, grid, kSumWarps * 32, s, a);
-  }
-  if (vec) return launch_after(k_embed_sum<Y, G, 8, false>, grid, kSumWarps * 32, s, a);
-  return launch_after(k_embed_sum<Y, G, 1, false>, grid, kSumWarps * 32, s, a);
+  auto launch = [&](auto add) -> cudaError_t {
+    constexpr bool kAdd = decltype(add)::value;
+    if (!vec) return launch_after(k_embed_sum<Y, G, 1, kAdd>, grid, kSumWarps * 32, 0, s, a);
+    constexpr int kShared = kSumWarps * Ring<Y, G, kAdd>::kBytes;
+    if (kShared > 48 * 1024) {
+      const cudaError_t e = cudaFuncSetAttribute(k_embed_sum<Y, G, 8, kAdd>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+      if (e != cudaSuccess) return e;
+    }
+    return launch_after(k_embed_sum<Y, G, 8, kAdd>, grid, kSumWarps * 32, kShared, s, a);
+  };
+  return a.accumulate ? launch(std::true_type{}) : launch(std::false_type{});
+}
+
+template <typename G>
+cudaError_t launch_join(const GradArgs &a, bool vec, cudaStream_t s) {
+  const int cols = vec ? 128 : 32, lengthy = a.blocks > kLong + 1 ? (a.D + cols - 1) / cols * kShare : 0;
+  const dim3 grid((unsigned)(a.blocks - 1 + lengthy), (unsigned)a.K);
+  return vec ? launch_after(k_embed_join<G, 4>, grid, kJoinThreads, 0, s, a) : launch_after(k_embed_join<G, 1>, grid, kJoinThreads, 0, s, a);
 }
 
 }  // namespace
@@ -660,7 +904,7 @@ dasgd_status dasgd_embed_workspace(const dasgd_embed_config *cfg, int64_t *bytes
   const dasgd_status st = check(cfg, "embed_workspace");
   if (st != DASGD_OK) return st;
   if (!bytes) return bad("embed_workspace: bytes is NULL");
-  *bytes = (int64_t)plan(*cfg).bytes;
+  *bytes = (int64_t)plan(*cfg, false).bytes;  // the same for either kind of slices
   return DASGD_OK;
 }
 
@@ -669,7 +913,8 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   dasgd_status st = check(cfg, "embed_gradient");
   if (st != DASGD_OK) return st;
   const dasgd_embed_config &c = *cfg;
-  const Plan p = plan(c);
+  const bool vec = wide(c, grad_array, dy);
+  const Plan p = plan(c, vec);
   if (c.T == 0 && c.accumulate) return DASGD_OK;
   if (!grad_array || (c.T && (!dy || !tokens))) return bad("embed_gradient: dy, tokens and grad_array must not be NULL");
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < (int64_t)p.bytes)
@@ -717,7 +962,6 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   a.part = reinterpret_cast<float *>(ws + p.part);
   a.ld = c.ld, a.T = c.T, a.V = c.V, a.D = c.D, a.K = c.K, a.blk = p.blk, a.blocks = p.blocks, a.slices = p.slices;
   a.scale = c.scale, a.accumulate = c.accumulate != 0;
-  const bool vec = wide(c, grad_array, dy);
   const bool y32 = c.rows_elem == DASGD_ELEM_F32, g32 = c.table_elem == DASGD_ELEM_F32;
   if (y32 && g32) e = launch_sum<float, float>(a, vec, sum_ctas, s);
   else if (y32) e = launch_sum<float, __nv_bfloat16>(a, vec, sum_ctas, s);
@@ -725,9 +969,7 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   else e = launch_sum<__nv_bfloat16, __nv_bfloat16>(a, vec, sum_ctas, s);
   if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sums");
   if (p.blocks > 1) {
-    const int lengthy = p.blocks > kLong + 1 ? (c.D + kJoinCols - 1) / kJoinCols : 0;
-    const dim3 grid((unsigned)(p.blocks - 1 + lengthy), (unsigned)c.K);
-    e = g32 ? launch_after(k_embed_join<float>, grid, kJoinThreads, s, a) : launch_after(k_embed_join<__nv_bfloat16>, grid, kJoinThreads, s, a);
+    e = g32 ? launch_join<float>(a, vec, s) : launch_join<__nv_bfloat16>(a, vec, s);
     if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: joining");
   }
   e = cudaGetLastError();

@@ -17,7 +17,7 @@ def _embed(**kw):
 @pytest.mark.parametrize("bad,frag", [
     (dict(K=0), "K must"), (dict(K=65536), "K must"), (dict(V=0), "V must"), (dict(D=0), "D must"), (dict(T=-1), "T must"), (dict(T=2 ** 31), "T must"),
     (dict(ld=83), "inside a row"), (dict(offset=-1), "inside a row"), (dict(offset=21), "inside a row"), (dict(token_bits=16), "token_bits"),
-    (dict(table_elem=2), "element type"), (dict(rows_elem=-1), "element type"), (dict(device=-1), "device"),
+    (dict(table_elem=2), "element type"), (dict(rows_elem=-1), "element type"), (dict(device=-1), "device"), (dict(scale=float("nan")), "scale"),
 ])
 def test_embedding_configuration_is_checked(bad, frag):
     c = _embed(**bad)
