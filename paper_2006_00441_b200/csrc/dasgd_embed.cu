@@ -70,6 +70,20 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   return *reinterpret_cast<const uint32_t *>(&v);
 }
 
+// Adds to VEC float32 in memory where they lie, without bringing them here.  Every element is added to once in a launch, so
+// the order in which the additions happen decides nothing.
+template <int VEC>
+__device__ __forceinline__ void add_in_place(float *p, const float (&x)[VEC]) {
+  if constexpr (VEC == 1) {
+    asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x[0]) : "memory");
+  } else {
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4)
+      asm volatile("red.relaxed.gpu.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                   ::"l"(p + i), "f"(x[i]), "f"(x[i + 1]), "f"(x[i + 2]), "f"(x[i + 3]) : "memory");
+  }
+}
+
 template <typename T, int VEC>
 __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {  // streaming: nothing here is read again
   if constexpr (VEC == 1) {
@@ -323,6 +337,7 @@ constexpr int kSumWarps = 2, kAhead = 4;
 template <typename Y, typename G, int VEC, bool ADD>
 __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   constexpr int NV = 8 / VEC;
+  constexpr bool kOld = ADD && sizeof(G) == 2;
   const int lane = threadIdx.x & 31;
   const int s = (int)(task % a.slices);
   const long long kb = task / a.slices;
@@ -354,13 +369,13 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
     for (int j0 = 0; j0 < n; j0 += kAhead) {
       if (__shfl_sync(0xffffffffu, kl, j0) == none) return;  // only tokens outside the table follow
       Raw<Y, VEC> x[kAhead][NV];
-      Raw<G, VEC> old[ADD ? kAhead : 1][NV];
+      Raw<G, VEC> old[kOld ? kAhead : 1][NV];
 #pragma unroll
       for (int j = 0; j < kAhead; ++j) {
         const Y *row = dy + (long long)__shfl_sync(0xffffffffu, pl, j0 + j) * a.D;  // row 0 past the end
 #pragma unroll
         for (int u = 0; u < NV; ++u) x[j][u].load(row + max(col[u], 0));
-        if constexpr (ADD) {
+        if constexpr (kOld) {
           const uint32_t kj = __shfl_sync(0xffffffffu, kl, j0 + j);
           if (__shfl_sync(0xffffffffu, what, j0 + j) == 1)
 #pragma unroll
@@ -388,10 +403,11 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
               store<float, VEC>(part + (head ? 0 : a.D) + col[u], acc[u]);
             } else {
               float v[VEC], o[VEC] = {};
-              if constexpr (ADD) old[j][u].widen(o);
+              if constexpr (kOld) old[j][u].widen(o);
 #pragma unroll
-              for (int i = 0; i < VEC; ++i) v[i] = ADD ? fmaf(a.scale, acc[u][i], o[i]) : __fmul_rn(a.scale, acc[u][i]);
-              store<G, VEC>(grad + (long long)kj * a.D + col[u], v);
+              for (int i = 0; i < VEC; ++i) v[i] = kOld ? fmaf(a.scale, acc[u][i], o[i]) : __fmul_rn(a.scale, acc[u][i]);
+              if constexpr (ADD && !kOld) add_in_place<VEC>(grad + (long long)kj * a.D + col[u], v);
+              else store<G, VEC>(grad + (long long)kj * a.D + col[u], v);
             }
           }
 #pragma unroll
@@ -408,9 +424,10 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
 // registers as many rows in flight would leave room for a third of the warps.
 template <typename Y, typename G, bool ADD>
 struct Ring {
-  static constexpr int kRows = ADD ? 8 : 16, kStep = ADD ? 2 : 4;  // rows of the ring; rows asked for, and waited for, together
+  static constexpr bool kAdds = ADD && sizeof(G) == 2;                 // bfloat16 rows that are added to come along; float32 ones stay where they are
+  static constexpr int kRows = kAdds ? 8 : 16, kStep = kAdds ? 2 : 4;  // rows of the ring; rows asked for, and waited for, together
   static constexpr int kUnits = kWideCols / 256;                   // units of 8 columns of a lane, 256 columns apart
-  static constexpr int kNew = kUnits * 8 * sizeof(Y) * 32 / 16, kOld = ADD ? kUnits * 8 * sizeof(G) * 32 / 16 : 0;  // 16-byte pieces of a row
+  static constexpr int kNew = kUnits * 8 * sizeof(Y) * 32 / 16, kOld = kAdds ? kUnits * 8 * sizeof(G) * 32 / 16 : 0;  // 16-byte pieces of a row
   static constexpr int kBytes = kRows * (kNew + kOld) * 16;
 };
 
@@ -483,7 +500,7 @@ __device__ __forceinline__ void sum_block_ring(const GradArgs &a, long long task
 #pragma unroll
         for (int u = 0; u < R::kUnits; ++u)
           if (mine[u]) copy8<Y>(to + u * (R::kNew / R::kUnits) * 16, row + u * 256);
-        if constexpr (ADD) {
+        if constexpr (R::kAdds) {
           if ((en.ends & ~en.goes) >> l & 1) {
             const G *old = grad + (long long)__shfl_sync(0xffffffffu, en.key, l) * a.D;
 #pragma unroll
@@ -528,10 +545,11 @@ __device__ __forceinline__ void sum_block_ring(const GradArgs &a, long long task
             store<float, 8>(part + (head ? 0 : a.D) + u * 256, acc[u]);
           } else {
             float v[8], o[8] = {};
-            if constexpr (ADD) read8<G>(row + R::kNew + u * (R::kOld / R::kUnits), o);
+            if constexpr (R::kAdds) read8<G>(row + R::kNew + u * (R::kOld / R::kUnits), o);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) v[c] = ADD ? fmaf(a.scale, acc[u][c], o[c]) : __fmul_rn(a.scale, acc[u][c]);
-            store<G, 8>(grad + kj * a.D + u * 256, v);
+            for (int c = 0; c < 8; ++c) v[c] = R::kAdds ? fmaf(a.scale, acc[u][c], o[c]) : __fmul_rn(a.scale, acc[u][c]);
+            if constexpr (ADD && !R::kAdds) add_in_place<8>(grad + kj * a.D + u * 256, v);
+            else store<G, 8>(grad + kj * a.D + u * 256, v);
           }
         }
 #pragma unroll
