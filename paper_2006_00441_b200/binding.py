@@ -372,7 +372,11 @@ _TOKEN_BITS = {torch.int32: 32, torch.int64: 64}
 
 
 class _StreamOrder:
-    """Calls that share a workspace run one after the other also when the caller changes streams between them."""
+    """Calls that share a workspace run one after the other also when the caller changes streams between them.
+
+    A stream that is being captured into a graph cannot wait for work outside the capture: there, and for the graph's
+    replays, the order is the caller's to keep.
+    """
 
     def __init__(self, device):
         self.device, self.index, self.done = device, device.index, None
@@ -383,11 +387,12 @@ class _StreamOrder:
         raw = torch._C._cuda_getCurrentRawStream(self.index)
         if raw != self.raw:
             stream = torch.cuda.current_stream(self.device)
-            if self.done is None:
-                self.done = torch.cuda.Event()
-            self.done.record(self.last)
-            stream.wait_event(self.done)
-            workspace.record_stream(stream)
+            if not torch.cuda.is_current_stream_capturing():
+                if self.done is None:
+                    self.done = torch.cuda.Event()
+                self.done.record(self.last)
+                stream.wait_event(self.done)
+                workspace.record_stream(stream)
             self.last, self.raw = stream, raw
         return raw
 

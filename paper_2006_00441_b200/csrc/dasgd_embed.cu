@@ -156,15 +156,16 @@ __global__ void __launch_bounds__(kThreads, 6) k_embed_lookup(const LookupArgs a
 
 struct SortArgs {
   const void *tokens;
-  uint32_t *key[2], *pos[2];  // [K][T] each; the sorted result is in [passes & 1]
+  uint2 *list[2];             // [K][T] entries (position, key) each; the sorted result is in [passes & 1]
   long long T;
   int V, token_bits, passes, radix_bits, K;
   int sorted;                 // replicas to sort: K, or 0 without tokens
-  char *grad;                 // the table's gradient, to be zeroed; NULL: left alone
-  long long grad_stride, grad_bytes;  // from replica to replica, of a replica
+  char *grad;                 // the table's gradient, of which grad_bytes of every replica are zeroed
+  long long grad_stride, grad_bytes;
 };
 
 constexpr int kZeroCtas = 148 * 3;    // with the sorting clusters in front they fill the SMs
+constexpr int kMaxCluster = 16;
 constexpr int kZeroPiece = 1 << 16;  // bytes that a CTA zeroes at a time
 
 __device__ __forceinline__ void zero_piece(char *p, int n) {  // n <= kZeroPiece bytes, an even number
@@ -184,10 +185,19 @@ __device__ __forceinline__ void zero_piece(char *p, int n) {  // n <= kZeroPiece
 //
 // Sorting keeps a few SMs busy with latencies.  The clusters after the first K meanwhile zero the whole table of every replica
 // (rows that tokens select are written once more by the sums: cheaper than waiting to know which).
+struct SortShared {
+  uint32_t hist[kSortWarps][kMaxRadix];    // counts of the warps' digits, then where their next entry of a digit goes
+  uint32_t total[kMaxCluster][kMaxRadix];  // of every CTA of the cluster, which writes it here
+  uint32_t scan[kSortWarps];
+};
+
+// kBatch: entries of a lane that are loaded and voted on together; a warp whose part is no longer than that holds it in
+// registers from the counting to the placing.
+template <int kBatch>
 __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) {
-  __shared__ uint32_t hist[kSortWarps][kMaxRadix];
-  __shared__ uint32_t total[kMaxRadix];
-  __shared__ uint32_t scan[kSortThreads / 32];
+  extern __shared__ __align__(16) uint8_t sort_shared[];
+  SortShared &sh = *reinterpret_cast<SortShared *>(sort_shared);
+  auto &hist = sh.hist;
   asm volatile("griddepcontrol.launch_dependents;");
   cg::cluster_group cluster = cg::this_cluster();
   const int nC = cluster.num_blocks(), rank = cluster.block_rank();
@@ -201,7 +211,6 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
     }
     return;
   }
-  constexpr int kBatch = 8;  // keys of a lane that are loaded together
   const int R = 1 << a.radix_bits;
   const uint32_t none = (uint32_t)a.V;
   const long long per = (a.T + nC - 1) / nC;                                   // positions of a CTA
@@ -210,16 +219,16 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
   const long long w0 = min(hi, lo + warp * seg), w1 = min(hi, w0 + seg);
 
   for (int pass = 0; pass < a.passes; ++pass) {
-    const uint32_t *kin = a.key[pass & 1] + k * a.T, *pin = a.pos[pass & 1] + k * a.T;
-    uint32_t *kout = a.key[(pass & 1) ^ 1] + k * a.T, *pout = a.pos[(pass & 1) ^ 1] + k * a.T;
+    const uint2 *from = a.list[pass & 1] + k * a.T;
+    uint2 *to = a.list[(pass & 1) ^ 1] + k * a.T;
     const int shift = pass * a.radix_bits;
-    uint32_t keys[kBatch];
-    auto load_keys = [&](long long base) {
+    uint2 entry[kBatch];
+    auto load_entries = [&](long long base) {
       if (pass) {
 #pragma unroll
         for (int r = 0; r < kBatch; ++r) {
           const long long i = base + r * 32 + lane;
-          keys[r] = i < w1 ? __ldcg(kin + i) : 0;
+          entry[r] = i < w1 ? __ldcg(from + i) : make_uint2(0, 0);
         }
       } else {
         long long t[kBatch];
@@ -229,20 +238,34 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
           t[r] = i < w1 ? token_at(a.tokens, a.token_bits, k * a.T + i) : 0;
         }
 #pragma unroll
-        for (int r = 0; r < kBatch; ++r) keys[r] = t[r] >= 0 && t[r] < a.V ? (uint32_t)t[r] : none;
+        for (int r = 0; r < kBatch; ++r)
+          entry[r] = make_uint2((uint32_t)(base + r * 32 + lane), t[r] >= 0 && t[r] < a.V ? (uint32_t)t[r] : none);
       }
     };
+    // the lanes that have the same digit in a round, bit by bit, for all rounds of the batch side by side: one round after the
+    // other waits for nine votes in turn, and __match_any_sync takes no less
+    unsigned same[kBatch];
+    auto find_same = [&](long long base) {
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) same[r] = __ballot_sync(0xffffffffu, base + r * 32 + lane < w1);
+      for (int i = shift; i < shift + a.radix_bits; ++i) {
+#pragma unroll
+        for (int r = 0; r < kBatch; ++r) {
+          const bool one = entry[r].y >> i & 1;
+          const unsigned ones = __ballot_sync(0xffffffffu, one);
+          same[r] &= one ? ones : ~ones;
+        }
+      }
+    };
+    const bool single = w1 - w0 <= kBatch * 32;  // the second sweep finds everything in registers
     for (int d = lane; d < R; d += 32) hist[warp][d] = 0;
     __syncwarp();
     for (long long base = w0; base < w1; base += kBatch * 32) {
-      load_keys(base);
+      load_entries(base);
+      find_same(base);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
-        if (base + r * 32 >= w1) break;
-        const bool in = base + r * 32 + lane < w1;
-        const uint32_t d = in ? (keys[r] >> shift) & (R - 1) : (uint32_t)R;
-        const unsigned same = __match_any_sync(0xffffffffu, d);
-        if (in && lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
+        if (base + r * 32 + lane < w1 && lane == __ffs(same[r]) - 1) hist[warp][entry[r].y >> shift & (R - 1)] += __popc(same[r]);
         __syncwarp();
       }
     }
@@ -255,18 +278,16 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
         hist[w][tid] = s;
         s += c;
       }
-      total[tid] = s;
+      for (int c = 0; c < nC; ++c) *cluster.map_shared_rank(&sh.total[rank][tid], c) = s;
     }
     cluster.sync();
     uint32_t before = 0, all = 0;
     if (tid < R) {
-      uint32_t n[8];  // a cluster has at most 8 CTAs
 #pragma unroll
-      for (int c = 0; c < 8; ++c) n[c] = c < nC ? *cluster.map_shared_rank(&total[tid], c) : 0;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) {
-        all += n[c];
-        if (c < rank) before += n[c];
+      for (int c = 0; c < kMaxCluster; ++c) {
+        const uint32_t n = c < nC ? sh.total[c][tid] : 0;
+        all += n;
+        if (c < rank) before += n;
       }
     }
     uint32_t incl = all;  // exclusive scan of `all` over the digits (threads beyond R hold 0)
@@ -275,40 +296,32 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
       const uint32_t n = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += n;
     }
-    if (lane == 31) scan[warp] = incl;
+    if (lane == 31) sh.scan[warp] = incl;
     __syncthreads();
     uint32_t base0 = incl - all + before;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) base0 += w < warp ? scan[w] : 0;
+    for (int w = 0; w < kSortWarps; ++w) base0 += w < warp ? sh.scan[w] : 0;
     if (tid < R)
 #pragma unroll
       for (int w = 0; w < kSortWarps; ++w) hist[w][tid] += base0;
     __syncthreads();
     for (long long base = w0; base < w1; base += kBatch * 32) {
-      load_keys(base);
-      uint32_t from[kBatch];
-#pragma unroll
-      for (int r = 0; r < kBatch; ++r) {
-        const long long i = base + r * 32 + lane;
-        from[r] = !pass ? (uint32_t)i : i < w1 ? __ldcg(pin + i) : 0;
+      if (!single) {
+        load_entries(base);
+        find_same(base);
       }
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
-        if (base + r * 32 >= w1) break;
         const bool in = base + r * 32 + lane < w1;
-        const uint32_t d = in ? (keys[r] >> shift) & (R - 1) : (uint32_t)R;
-        const unsigned same = __match_any_sync(0xffffffffu, d);
-        if (in) {
-          const uint32_t at = hist[warp][d] + __popc(same & ((1u << lane) - 1));
-          kout[at] = keys[r];
-          pout[at] = from[r];
-        }
+        const uint32_t d = entry[r].y >> shift & (R - 1);
+        const uint32_t at = hist[warp][d];
         __syncwarp();
-        if (in && lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
+        if (in && lane == __ffs(same[r]) - 1) hist[warp][d] = at + __popc(same[r]);
         __syncwarp();
+        if (in) to[at + __popc(same[r] & ((1u << lane) - 1))] = entry[r];
       }
     }
-    cluster.sync();  // the next pass reads what other CTAs wrote, and `total` may be overwritten
+    cluster.sync();  // the next pass reads what other CTAs wrote, and the totals may be overwritten
   }
 }
 
@@ -317,7 +330,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
 struct GradArgs {
   const void *dy;             // [K][T][D]
   void *grad;                 // already moved to the table's first element
-  const uint32_t *key, *pos;  // [K][T], sorted
+  const uint2 *list;          // [K][T] entries (position, key), sorted by key, then by position
   float *part;                // [K][blocks][2][D]: sums of runs that cross the borders of a block
   long long ld, T;
   int V, D, K;
@@ -344,9 +357,9 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   const int b = (int)(kb % a.blocks);
   const long long k = kb / a.blocks;
   const uint32_t none = (uint32_t)a.V;
-  const uint32_t *key = a.key + k * a.T, *pos = a.pos + k * a.T;
+  const uint2 *list = a.list + k * a.T;
   const long long e0 = (long long)b * a.blk, e1 = min(a.T, e0 + a.blk);
-  const uint32_t first = key[e0], prev = e0 ? key[e0 - 1] : none, next = e1 < a.T ? key[e1] : none;
+  const uint32_t first = list[e0].y, prev = e0 ? list[e0 - 1].y : none, next = e1 < a.T ? list[e1].y : none;
   if (first == none) return;
   const int c0 = s * kSliceCols + lane * VEC;
   int col[NV];  // this lane's columns; the ones beyond D are read at column 0 and not written
@@ -360,9 +373,10 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   bool head = prev == first;  // the first run of the block began earlier
   for (long long e = e0; e < e1; e += 32) {
     const int n = (int)min(32LL, e1 - e);
-    const uint32_t kl = lane < n ? key[e + lane] : none, pl = lane < n ? pos[e + lane] : 0;
+    const uint2 entry = lane < n ? list[e + lane] : make_uint2(0, none);
+    const uint32_t kl = entry.y, pl = entry.x;
     uint32_t follow = __shfl_down_sync(0xffffffffu, kl, 1);
-    if (lane == 31) follow = e + 32 < e1 ? key[e + 32] : none;
+    if (lane == 31) follow = e + 32 < e1 ? list[e + 32].y : none;
     const bool last = e + lane == e1 - 1;
     // what an entry does when it has been added: 0 nothing, 1 its run ends in the block, 2 its run goes on in the next one
     const int what = kl == none || (!last && follow == kl) ? 0 : last && next == kl ? 2 : 1;
@@ -455,9 +469,9 @@ __device__ __forceinline__ void sum_block_ring(const GradArgs &a, long long task
   const int b = (int)(kb % a.blocks);
   const long long k = kb / a.blocks;
   const uint32_t none = (uint32_t)a.V;
-  const uint32_t *key = a.key + k * a.T, *pos = a.pos + k * a.T;
+  const uint2 *list = a.list + k * a.T;
   const long long e0 = (long long)b * a.blk, e1 = min(a.T, e0 + a.blk);
-  const uint32_t first = key[e0], prev = e0 ? key[e0 - 1] : none, next = e1 < a.T ? key[e1] : none;
+  const uint32_t first = list[e0].y, prev = e0 ? list[e0 - 1].y : none, next = e1 < a.T ? list[e1].y : none;
   const int c0 = s * kWideCols + lane * 8;
   const Y *dy = static_cast<const Y *>(a.dy) + k * a.T * a.D + c0;
   G *grad = static_cast<G *>(a.grad) + k * a.ld + c0;
@@ -476,9 +490,10 @@ __device__ __forceinline__ void sum_block_ring(const GradArgs &a, long long task
   auto fetch = [&](long long e) {
     const long long i = e + lane;
     Entries r;
-    r.key = i < e1 ? key[i] : none, r.pos = i < e1 ? pos[i] : 0;
+    const uint2 entry = i < e1 ? list[i] : make_uint2(0, none);
+    r.key = entry.y, r.pos = entry.x;
     uint32_t follow = __shfl_down_sync(0xffffffffu, r.key, 1);
-    if (lane == 31) follow = i + 1 < e1 ? key[i + 1] : none;
+    if (lane == 31) follow = i + 1 < e1 ? list[i + 1].y : none;
     const bool last = i == e1 - 1;
     r.here = __ballot_sync(0xffffffffu, r.key != none);
     r.ends = __ballot_sync(0xffffffffu, r.key != none && (last || follow != r.key));
@@ -588,12 +603,12 @@ struct Run {
   bool lengthy; // it reaches beyond the kLong blocks after this one
 };
 
-__device__ __forceinline__ Run crossing(const GradArgs &a, const uint32_t *key, int b) {
+__device__ __forceinline__ Run crossing(const GradArgs &a, const uint2 *list, int b) {
   const long long e0 = (long long)b * a.blk, e1 = e0 + a.blk, far = e1 + (long long)kLong * a.blk;
   Run r{(uint32_t)a.V, false};
   if (e1 >= a.T) return r;
-  const uint32_t v = key[e1 - 1], next = key[e1], first = key[e0], prev = e0 ? key[e0 - 1] : (uint32_t)a.V;
-  const uint32_t away = far < a.T ? key[far] : (uint32_t)a.V;
+  const uint32_t v = list[e1 - 1].y, next = list[e1].y, first = list[e0].y, prev = e0 ? list[e0 - 1].y : (uint32_t)a.V;
+  const uint32_t away = far < a.T ? list[far].y : (uint32_t)a.V;
   if (v == (uint32_t)a.V || next != v || (first == v && prev == v)) return r;
   r.v = v, r.lengthy = away == v;
   return r;
@@ -644,7 +659,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const long long k = blockIdx.y;
-  const uint32_t *key = a.key + k * a.T;
+  const uint2 *list = a.list + k * a.T;
   G *grad = static_cast<G *>(a.grad) + k * a.ld;
   const int short_ctas = a.blocks - 1;
   // part i of a run that begins in block b: slot 1 of block b for i = 0, slot 0 of block b + i after it
@@ -653,8 +668,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
   if (blockIdx.x < short_ctas) {
     const int b = blockIdx.x;
     const long long e = (long long)(b + 1 + lane) * a.blk;  // kLong < 32 blocks after this one
-    const uint32_t after = e < a.T ? key[e] : (uint32_t)a.V;
-    const Run r = crossing(a, key, b);
+    const uint32_t after = e < a.T ? list[e].y : (uint32_t)a.V;
+    const Run r = crossing(a, list, b);
     if (r.v == (uint32_t)a.V || r.lengthy) return;
     const int n = __ffs(~__ballot_sync(0xffffffffu, after == r.v));  // parts: one and those after it
     const float *part = parts(b);
@@ -682,7 +697,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
   const int unit = blockIdx.x - short_ctas, c = (unit / kShare) * 32 * VEC + lane * VEC;
   int number = 0;
   for (int from = 0; from < short_ctas; from += kJoinThreads) {
-    const bool hit = from + tid < short_ctas && crossing(a, key, from + tid).lengthy;
+    const bool hit = from + tid < short_ctas && crossing(a, list, from + tid).lengthy;
     const unsigned hits = __ballot_sync(0xffffffffu, hit);
     if (lane == 0) counts[warp] = __popc(hits);
     __syncthreads();
@@ -696,11 +711,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
     for (int f = 0; f < all; ++f) {
       if ((number + f) % kShare != unit % kShare) continue;
       const int b = found[f];
-      const uint32_t v = key[(long long)b * a.blk + a.blk - 1];
+      const uint32_t v = list[(long long)b * a.blk + a.blk - 1].y;
       int lo = b + kLong + 1, hi = a.blocks;  // the last block whose first token is v: binary search, the tokens are sorted
       while (hi - lo > 1) {
         const int mid = (lo + hi) / 2;
-        if (key[(long long)mid * a.blk] == v) lo = mid;
+        if (list[(long long)mid * a.blk].y == v) lo = mid;
         else hi = mid;
       }
       const int n = lo - b + 1;
@@ -785,7 +800,7 @@ bool wide(const dasgd_embed_config &c, const void *array, const void *rows) {
 
 struct Plan {  // of the gradient's workspace
   int blk, blocks, slices, passes, radix_bits, cluster;
-  size_t key[2], pos[2], part, bytes;
+  size_t list[2], part, bytes;
 };
 
 // Blocks of sorted tokens.  All warps that fit the SMs at once get one block of equal length, so that none is left to run alone
@@ -810,6 +825,15 @@ long long most_blocks(long long tasks, int warps) {  // tasks: replicas * slices
   return fit >= kWaves ? fit : (kWaves * (long long)kSms * warps + tasks - 1) / tasks;
 }
 
+// CTAs that sort a replica: one round of 32 tokens for every warp, up to 8 CTAs; two rounds before it becomes 16 (an opt-in
+// size), whose barriers take 2500 cycles against 1000.  8 x 8192 tokens: 29 us with 8 CTAs, 31 with 16; 4 x 16384: 33 and 32;
+// 4 x 32768: 48 and 45 (whole calls, rows of 8).
+int cluster_of(long long T) {
+  int n = 1;
+  while (n < 8 && T > (long long)n * kSortThreads) n *= 2;
+  return T > 16LL * kSortThreads ? kMaxCluster : n;
+}
+
 Plan plan(const dasgd_embed_config &c, bool vec) {
   Plan p;
   const int cols = vec ? kWideCols : kSliceCols;
@@ -826,15 +850,14 @@ Plan plan(const dasgd_embed_config &c, bool vec) {
   while (bits < 31 && (1LL << bits) <= c.V) ++bits;  // keys 0..V
   p.passes = (bits + kMaxRadixBits - 1) / kMaxRadixBits;
   p.radix_bits = (bits + p.passes - 1) / p.passes;
-  p.cluster = c.T <= 1024 ? 1 : c.T <= 2048 ? 2 : c.T <= 4096 ? 4 : 8;
+  p.cluster = cluster_of(c.T);
   size_t at = 0;
   auto take = [&](size_t n) {
     const size_t o = at;
     at += (n + 255) / 256 * 256;
     return o;
   };
-  const size_t list = (size_t)c.K * c.T * 4;
-  for (int i = 0; i < 2; ++i) p.key[i] = take(list), p.pos[i] = take(list);
+  for (int i = 0; i < 2; ++i) p.list[i] = take((size_t)c.K * c.T * sizeof(uint2));
   p.part = take((size_t)c.K * most * 2 * c.D * 4);
   p.bytes = at;
   return p;
@@ -949,10 +972,7 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
 
   SortArgs so{};
   so.tokens = tokens;
-  for (int i = 0; i < 2; ++i) {
-    so.key[i] = reinterpret_cast<uint32_t *>(ws + p.key[i]);
-    so.pos[i] = reinterpret_cast<uint32_t *>(ws + p.pos[i]);
-  }
+  for (int i = 0; i < 2; ++i) so.list[i] = reinterpret_cast<uint2 *>(ws + p.list[i]);
   so.T = c.T, so.V = c.V, so.token_bits = c.token_bits, so.passes = p.passes, so.radix_bits = p.radix_bits;
   so.K = c.K, so.sorted = c.T ? c.K : 0;
   char *grad = static_cast<char *>(grad_array) + c.offset * size_of(c.table_elem);
@@ -969,14 +989,19 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = p.cluster, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
   lc.attrs = attr, lc.numAttrs = 1;
-  cudaError_t e = cudaLaunchKernelEx(&lc, k_sort_tokens, so);
+  lc.dynamicSmemBytes = sizeof(SortShared);
+  const long long rounds = (c.T + (long long)p.cluster * kSortThreads - 1) / ((long long)p.cluster * kSortThreads);
+  auto kernel = rounds <= 1 ? k_sort_tokens<1> : rounds <= 2 ? k_sort_tokens<2> : rounds <= 4 ? k_sort_tokens<4> : k_sort_tokens<8>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortShared));
+  if (e == cudaSuccess && p.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) e = cudaLaunchKernelEx(&lc, kernel, so);
   if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sort");
   if (!c.T) return DASGD_OK;
 
   GradArgs a{};
   a.dy = dy;
   a.grad = grad;
-  a.key = so.key[p.passes & 1], a.pos = so.pos[p.passes & 1];
+  a.list = so.list[p.passes & 1];
   a.part = reinterpret_cast<float *>(ws + p.part);
   a.ld = c.ld, a.T = c.T, a.V = c.V, a.D = c.D, a.K = c.K, a.blk = p.blk, a.blocks = p.blocks, a.slices = p.slices;
   a.scale = c.scale, a.accumulate = c.accumulate != 0;
