@@ -71,7 +71,7 @@ struct Shape {                                            // matrices of one sha
 
 struct Group : Shape {                                    // and the kernels before them
   int matrices, ldx;                                      // row stride (elements) of X
-  int chunks, chunk0;                                     // pieces of a matrix in the momentum kernel; first piece of the group
+  int piece, chunks, chunk0;                              // elements of a piece of the momentum kernel, pieces of a matrix; first piece of the group
   int rblk, rblks, rblk0;                                 // rows of a piece, pieces, first piece in the scaling kernel
   __half *x[2][2], *a[2], *b[2];                          // [buffer][part], [part]
 };
@@ -95,7 +95,11 @@ struct Plan {                                             // kernel argument
 
 // ---------------------------------------------------------------- momentum and norm
 
-constexpr int kPrepThreads = 256, kChunk = 16384;
+// Both kernels before the products are bound by HBM: 10 or 12 bytes an element for the first (gradient, momentum array in and
+// out), 6 or 8 and 4 written for the second.  The second takes its pieces from the last to the first, so that what the first
+// kernel touched last is still in L2.
+constexpr int kPrepThreads = 256, kBatch = 16;             // elements that a thread has in flight
+constexpr int kPiece = kPrepThreads * kBatch;              // the least work of a CTA; four times that for matrices of 2^20 entries and more
 
 template <typename T>
 __device__ __forceinline__ float to_f(T v) { return static_cast<float>(v); }
@@ -124,42 +128,63 @@ __device__ __forceinline__ int group_of(const Plan &p, int at, int Group::*first
 template <typename T>
 __global__ void __launch_bounds__(kPrepThreads) k_ortho_momentum(const Plan p, const T *g, float *m, int vec) {
   __shared__ double part[kPrepThreads / 32];
+  asm volatile("griddepcontrol.launch_dependents;");
   for (int i = blockIdx.x * kPrepThreads + threadIdx.x; i < p.n_done; i += gridDim.x * kPrepThreads) p.done[i] = 0;
   const Group &gr = p.groups[group_of(p, blockIdx.x, &Group::chunk0)];
   const int local = blockIdx.x - gr.chunk0, z = local / gr.chunks, c = local % gr.chunks;
-  const long long numel = (long long)gr.rows * gr.cols, lo = (long long)c * kChunk, hi = min(numel, lo + kChunk);
+  const long long numel = (long long)gr.rows * gr.cols, lo = (long long)c * gr.piece, hi = min(numel, lo + gr.piece);
   const long long base = (z % p.K) * p.ld + p.offset[gr.m0 + z / p.K];
   const T *gp = g + base;
   float *mp = m ? m + base : nullptr;
   float s = 0.f;
-  long long e = lo;
+  long long e0 = lo;
   if (vec && gr.even) {
-    for (e = lo + threadIdx.x * 8; e + 8 <= hi; e += kPrepThreads * 8) {
-      float x[8];
-      load8(gp + e, x);
-      if (mp) {
-        float o[8];
-        load8(mp + e, o);
+    const long long end = lo + (hi - lo) / 8 * 8;
+    for (long long e = lo + threadIdx.x * 8; e < end; e += kPiece) {
+      // loads first: past the end the first one's place is read again, and nothing written
+      long long at[kBatch / 8];
+      float x[kBatch / 8][8], o[kBatch / 8][8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = fmaf(p.mu, o[i], x[i]);
-        *reinterpret_cast<float4 *>(mp + e) = make_float4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<float4 *>(mp + e + 4) = make_float4(o[4], o[5], o[6], o[7]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = direction(x[i], o[i], p.mu, p.nesterov);
+      for (int h = 0; h < kBatch / 8; ++h) {
+        at[h] = e + h * (kPrepThreads * 8);
+        load8(gp + (at[h] < end ? at[h] : e), x[h]);
+        if (mp) load8(mp + (at[h] < end ? at[h] : e), o[h]);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+      for (int h = 0; h < kBatch / 8; ++h) {
+        if (at[h] >= end) continue;
+        if (mp) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[h][i] = fmaf(p.mu, o[h][i], x[h][i]);
+          *reinterpret_cast<float4 *>(mp + at[h]) = make_float4(o[h][0], o[h][1], o[h][2], o[h][3]);
+          *reinterpret_cast<float4 *>(mp + at[h] + 4) = make_float4(o[h][4], o[h][5], o[h][6], o[h][7]);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[h][i] = direction(x[h][i], o[h][i], p.mu, p.nesterov);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(x[h][i], x[h][i], s);
+      }
     }
-    e = lo + (hi - lo) / 8 * 8;
+    e0 = end;
   }
-  for (e += threadIdx.x; e < hi; e += kPrepThreads) {
-    float x = to_f(gp[e]);
-    if (mp) {
-      const float o = fmaf(p.mu, mp[e], x);
-      mp[e] = o;
-      x = direction(x, o, p.mu, p.nesterov);
+  for (long long e = e0 + threadIdx.x; e < hi; e += kPiece) {
+    float x[kBatch], o[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const long long at = min(e + i * kPrepThreads, hi - 1);
+      x[i] = to_f(gp[at]);
+      o[i] = mp ? mp[at] : 0.f;
     }
-    s = fmaf(x, x, s);
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (e + i * kPrepThreads >= hi) break;
+      if (mp) {
+        o[i] = fmaf(p.mu, o[i], x[i]);
+        mp[e + i * kPrepThreads] = o[i];
+        x[i] = direction(x[i], o[i], p.mu, p.nesterov);
+      }
+      s = fmaf(x[i], x[i], s);
+    }
   }
   double d = s;
 #pragma unroll
@@ -180,8 +205,10 @@ __device__ __forceinline__ uint32_t pack_half(__half a, __half b) {
 template <typename T>
 __global__ void __launch_bounds__(kPrepThreads) k_ortho_scale(const Plan p, const T *g, const float *m, int vec) {
   __shared__ double part[kPrepThreads / 32];
-  const Group &gr = p.groups[group_of(p, blockIdx.x, &Group::rblk0)];
-  const int local = blockIdx.x - gr.rblk0, z = local / gr.rblks, r0 = local % gr.rblks * gr.rblk;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int block = gridDim.x - 1 - blockIdx.x;
+  const Group &gr = p.groups[group_of(p, block, &Group::rblk0)];
+  const int local = block - gr.rblk0, z = local / gr.rblks, r0 = local % gr.rblks * gr.rblk;
   double d = 0.0;
   for (int i = threadIdx.x; i < gr.chunks; i += kPrepThreads) d += p.sumsq[gr.chunk0 + z * gr.chunks + i];
 #pragma unroll
@@ -196,40 +223,49 @@ __global__ void __launch_bounds__(kPrepThreads) k_ortho_scale(const Plan p, cons
   const T *gp = g + base;
   const float *mp = m ? m + base : nullptr;
   const long long xbase = (long long)z * gr.rows * gr.ldx;
-  const int units = gr.ldx / 8, r1 = min(gr.rows, r0 + gr.rblk);
-  for (int i = threadIdx.x; i < (r1 - r0) * units; i += kPrepThreads) {
-    const int r = r0 + i / units, c = i % units * 8;
-    const long long at = (long long)r * gr.cols + c;
-    float x[8];
-    if (vec && gr.even == 2 && c + 8 <= gr.cols) {
-      load8(gp + at, x);
-      if (mp) {
-        float o[8];
-        load8(mp + at, o);
+  const int units = gr.ldx / 8, all = (min(gr.rows, r0 + gr.rblk) - r0) * units;  // units of 8 columns
+  const bool even = vec && gr.even == 2;
+  for (int i0 = threadIdx.x; i0 < all; i0 += kPiece / 8) {
+    float x[kBatch / 8][8], o[kBatch / 8][8];
+    int row[kBatch / 8], col[kBatch / 8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = direction(x[j], o[j], p.mu, p.nesterov);
-      }
-    } else {
+    for (int h = 0; h < kBatch / 8; ++h) {
+      const int i = min(i0 + h * kPrepThreads, all - 1);
+      row[h] = r0 + i / units, col[h] = i % units * 8;
+      const long long at = (long long)row[h] * gr.cols + col[h];
+      if (even) {  // rows are multiples of 8 long: a unit is inside or outside
+        const long long in = col[h] < gr.cols ? at : 0;
+        load8(gp + in, x[h]);
+        if (mp) load8(mp + in, o[h]);
+      } else {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        x[j] = 0.f;
-        if (c + j < gr.cols) {
-          x[j] = to_f(gp[at + j]);
-          if (mp) x[j] = direction(x[j], mp[at + j], p.mu, p.nesterov);
+        for (int j = 0; j < 8; ++j) {
+          const long long in = col[h] + j < gr.cols ? at + j : 0;
+          x[h][j] = to_f(gp[in]);
+          o[h][j] = mp ? mp[in] : 0.f;
         }
       }
     }
-    uint32_t h[4], l[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float a = x[2 * j] * f, b = x[2 * j + 1] * f;
-      const __half ha = __float2half_rn(a), hb = __float2half_rn(b);
-      h[j] = pack_half(ha, hb);
-      l[j] = pack_half(__float2half_rn(a - __half2float(ha)), __float2half_rn(b - __half2float(hb)));
+    for (int h = 0; h < kBatch / 8; ++h) {
+      if (i0 + h * kPrepThreads >= all) break;
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float v[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const float u = mp ? direction(x[h][2 * j + q], o[h][2 * j + q], p.mu, p.nesterov) : x[h][2 * j + q];
+          v[q] = col[h] + 2 * j + q < gr.cols ? u * f : 0.f;
+        }
+        const __half ha = __float2half_rn(v[0]), hb = __float2half_rn(v[1]);
+        hi[j] = pack_half(ha, hb);
+        lo[j] = pack_half(__float2half_rn(v[0] - __half2float(ha)), __float2half_rn(v[1] - __half2float(hb)));
+      }
+      const long long to = xbase + (long long)row[h] * gr.ldx + col[h];
+      *reinterpret_cast<uint4 *>(gr.x[0][0] + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      *reinterpret_cast<uint4 *>(gr.x[0][1] + to) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
-    const long long o = xbase + (long long)r * gr.ldx + c;
-    *reinterpret_cast<uint4 *>(gr.x[0][0] + o) = make_uint4(h[0], h[1], h[2], h[3]);
-    *reinterpret_cast<uint4 *>(gr.x[0][1] + o) = make_uint4(l[0], l[1], l[2], l[3]);
   }
 }
 
@@ -258,9 +294,11 @@ __device__ __forceinline__ uint32_t mapped(uint32_t addr, int rank) {
   return a;
 }
 
-// arrives on the barrier at the same offset in CTA `rank` of the cluster
-__device__ __forceinline__ void mbar_arrive(uint32_t bar, int rank) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped(bar, rank)) : "memory");
+// arrives on the barrier at the same offset in the first CTA of the pair, or on this CTA's own
+template <int CG>
+__device__ __forceinline__ void mbar_arrive(uint32_t bar) {
+  if constexpr (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped(bar, 0)) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
@@ -874,7 +912,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       auto release = [&]() {      // it has been read
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (elected()) mbar_arrive(smem_u32(&sh.acc_empty[n & 1]), 0);
+        if (elected()) mbar_arrive<CG>(smem_u32(&sh.acc_empty[n & 1]));
         ++n;
       };
       bring(0);
@@ -1037,8 +1075,9 @@ dasgd_status layout(const dasgd_ortho_config *c, const char *who, int cg, Layout
     const long long tg = (long long)g.tn * (g.tn + 1) / 2, tu = (long long)g.tn * g.tw;
     g.ldx = (g.cols + 63) / 64 * 64, g.lda = (g.n + 63) / 64 * 64;
     const long long numel = (long long)g.rows * g.cols;
-    const long long pieces = (numel + kChunk - 1) / kChunk;
-    g.rblk = std::max(1, kChunk / g.ldx);
+    g.piece = numel < (1 << 20) ? kPiece : 4 * kPiece;
+    const long long pieces = (numel + g.piece - 1) / g.piece;
+    g.rblk = std::max(1, g.piece / g.ldx);
     g.rblks = (g.rows + g.rblk - 1) / g.rblk;
     // a matrix's finished epilogue warps are counted in 32 bits, its tiles and pieces in int
     if (tu >= (1 << 24) || pieces >= (1 << 30) || batch >= (1 << 30) || chunks + pieces * batch >= (1LL << 31) || rblks + g.rblks * batch >= (1LL << 31) ||
@@ -1176,9 +1215,15 @@ template <typename T>
 dasgd_status run(const dasgd_ortho *op, const T *g, float *m, T *out, cudaStream_t s) {
   const int vec = op->plan.ld % 8 == 0 && aligned(g, 16) && aligned(m, 16), vec_out = op->plan.ld % 8 == 0 && aligned(out, 16);
   k_ortho_momentum<T><<<op->chunks, kPrepThreads, 0, s>>>(op->plan, g, m, vec);
-  k_ortho_scale<T><<<op->rblks, kPrepThreads, 0, s>>>(op->plan, g, m, vec);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return cuda_fail(e, "ortho_step");
+  cudaLaunchConfig_t scale{};  // set up while the kernel before it runs
+  cudaLaunchAttribute after[1];
+  after[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  after[0].val.programmaticStreamSerializationAllowed = 1;
+  scale.gridDim = dim3(op->rblks), scale.blockDim = dim3(kPrepThreads), scale.stream = s, scale.attrs = after, scale.numAttrs = 1;
+  if ((e = cudaLaunchKernelEx(&scale, k_ortho_scale<T>, op->plan, g, static_cast<const float *>(m), vec)) != cudaSuccess)
+    return cuda_fail(e, "ortho_step");
   return with_kernel(op->cg, op->dtype, [&](auto kernel, auto *type) -> dasgd_status {
     using Out = std::remove_pointer_t<decltype(type)>;
     if constexpr (std::is_same_v<Out, T>) {
