@@ -201,6 +201,20 @@ __device__ __forceinline__ uint32_t pack_half(__half a, __half b) {
   return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16;
 }
 
+// The direction with what its rounding to float32 left out: weak directions of a matrix are amplified, and this with them.
+struct Exact {
+  float u, e;
+};
+__device__ __forceinline__ Exact exact_direction(float g, float m, float mu, int nesterov) {
+  if (!nesterov) return {m, 0.f};
+  const float p = __fmul_rn(mu, m), pe = fmaf(mu, m, -p);  // mu m = p + pe
+  const float u = __fadd_rn(g, p), b = __fsub_rn(u, g);    // g + p = u + the rest, which is exact
+  return {u, __fadd_rn(__fadd_rn(__fsub_rn(g, __fsub_rn(u, b)), __fsub_rn(p, b)), pe)};
+}
+
+// (u + e) * f beyond its leading fp16
+__device__ __forceinline__ __half rest_of(Exact x, float f, __half lead) { return __float2half_rn(fmaf(x.e, f, fmaf(x.u, f, -__half2float(lead)))); }
+
 // X_0 as a pair of fp16, the padding of its rows zeroed.
 template <typename T>
 __global__ void __launch_bounds__(kPrepThreads) k_ortho_scale(const Plan p, const T *g, const float *m, int vec) {
@@ -252,15 +266,15 @@ __global__ void __launch_bounds__(kPrepThreads) k_ortho_scale(const Plan p, cons
       uint32_t hi[4], lo[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        float v[2];
+        Exact u[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-          const float u = mp ? direction(x[h][2 * j + q], o[h][2 * j + q], p.mu, p.nesterov) : x[h][2 * j + q];
-          v[q] = col[h] + 2 * j + q < gr.cols ? u * f : 0.f;
+          u[q] = mp ? exact_direction(x[h][2 * j + q], o[h][2 * j + q], p.mu, p.nesterov) : Exact{x[h][2 * j + q], 0.f};
+          if (col[h] + 2 * j + q >= gr.cols) u[q] = Exact{0.f, 0.f};
         }
-        const __half ha = __float2half_rn(v[0]), hb = __float2half_rn(v[1]);
+        const __half ha = __float2half_rn(u[0].u * f), hb = __float2half_rn(u[1].u * f);
         hi[j] = pack_half(ha, hb);
-        lo[j] = pack_half(__float2half_rn(v[0] - __half2float(ha)), __float2half_rn(v[1] - __half2float(hb)));
+        lo[j] = pack_half(rest_of(u[0], f, ha), rest_of(u[1], f, hb));
       }
       const long long to = xbase + (long long)row[h] * gr.ldx + col[h];
       *reinterpret_cast<uint4 *>(gr.x[0][0] + to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -559,7 +573,7 @@ __device__ __forceinline__ void unpack(const uint4 &v, float (&x)[8]) {
 }
 
 // 8 entries: as fp16 and, where a second part is kept, the rest as fp16 again
-template <bool PAIR>
+template <bool PAIR, size_t PART = kStagePart>
 __device__ __forceinline__ void put(uint8_t *stage, int r, int c, const float *v) {
   uint32_t h[4], l[4];
 #pragma unroll
@@ -573,15 +587,15 @@ __device__ __forceinline__ void put(uint8_t *stage, int r, int c, const float *v
     }
   }
   *piece(stage, r, c) = make_uint4(h[0], h[1], h[2], h[3]);
-  if constexpr (PAIR) *piece(stage + kStagePart, r, c) = make_uint4(l[0], l[1], l[2], l[3]);
+  if constexpr (PAIR) *piece(stage + PART, r, c) = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-template <bool PAIR>
+template <bool PAIR, size_t PART = kStagePart>
 __device__ __forceinline__ void get(uint8_t *stage, int r, int c, float (&x)[8]) {
   unpack(*piece(stage, r, c), x);
   if constexpr (PAIR) {
     float y[8];
-    unpack(*piece(stage + kStagePart, r, c), y);
+    unpack(*piece(stage + PART, r, c), y);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] += y[i];
   }
@@ -970,6 +984,218 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   if (warp == 2) tmem_free<CG>(tmem, 2 * kCols);
 }
 
+// ---------------------------------------------------------------- small matrices: a CTA each, everything in its SM
+
+// A matrix of at most 128 x 256 fits an SM: the pair of X in 64-wide boxes of 128 rows, A (then, in its place, B) likewise.  One
+// kernel does momentum, norm, all steps and the result; a product waits for the one before it through a barrier of the CTA, not
+// through device memory, which takes a tile kernel 7000 cycles from product to product.  A matrix with more rows than columns is
+// held transposed.
+constexpr int kSmallN = 128, kSmallW = 256, kSmallWarps = 8, kSmallThreads = kSmallWarps * 32;
+constexpr int kTall = 128 * 128;  // bytes of a box of 128 rows
+
+struct SmallShared {
+  uint8_t x[2][kSmallW / 64][kTall];
+  uint8_t a[2][kSmallN / 64][kTall];
+  float da[kSmallN], db[kSmallN];
+  double part[kSmallWarps];
+  uint64_t done;
+  uint32_t tmem;
+  volatile int abort;
+};
+static_assert(sizeof(SmallShared) <= 227 * 1024, "shared memory of a CTA");
+
+template <bool SPLIT, typename T>
+__global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const Plan p, const T *g, float *m, T *out) {
+  extern __shared__ __align__(1024) uint8_t raw[];
+  SmallShared &sh = *reinterpret_cast<SmallShared *>(raw);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  if (smem_u32(raw) & 1023) {  // the swizzles below need it; nothing has started yet
+    if (tid == 0) atomicExch(p.error, 1);
+    return;
+  }
+  int gi = 0;
+  while (gi + 1 < p.n_groups && (int)blockIdx.x >= p.shapes[gi + 1].z0) ++gi;
+  const Shape sp = p.shapes[gi];
+  const int z = blockIdx.x - sp.z0, numel = sp.rows * sp.cols, boxes = (sp.w + 63) / 64, wsteps = (sp.w + 15) / 16, nsteps = (sp.n + 15) / 16;
+  const long long base = (z % p.K) * p.ld + p.offset[sp.m0 + z / p.K];
+  if (warp == 0) tmem_alloc<1>(smem_u32(&sh.tmem), 256);
+  if (tid == 0) {
+    mbar_init(smem_u32(&sh.done), 1);
+    sh.abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  for (int i = tid; i < 2 * boxes * (kTall / 16); i += kSmallThreads)
+    reinterpret_cast<uint4 *>(sh.x[i / (boxes * (kTall / 16))])[i % (boxes * (kTall / 16))] = make_uint4(0, 0, 0, 0);
+
+  // momentum and norm
+  const T *gp = g + base;
+  float *mp = m ? m + base : nullptr;
+  float s = 0.f;
+  for (int e = tid; e < numel; e += kSmallThreads * kBatch) {
+    float x[kBatch], o[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = min(e + i * kSmallThreads, numel - 1);
+      x[i] = to_f(gp[at]);
+      o[i] = mp ? mp[at] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (e + i * kSmallThreads >= numel) break;
+      if (mp) {
+        o[i] = fmaf(p.mu, o[i], x[i]);
+        mp[e + i * kSmallThreads] = o[i];
+        x[i] = direction(x[i], o[i], p.mu, p.nesterov);
+      }
+      s = fmaf(x[i], x[i], s);
+    }
+  }
+  double d = s;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if (lane == 0) sh.part[warp] = d;
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = sh.tmem;
+  d = 0.0;
+#pragma unroll
+  for (int i = 0; i < kSmallWarps; ++i) d += sh.part[i];
+  const float f = (float)((double)kStore / (sqrt(d) + (double)p.eps));
+  // X_0: every thread takes up the entries that it has just written
+  auto place = [&](int i, int j) { return (j >> 6) * kTall + i * 128 + (((j >> 3 & 7) ^ (i & 7)) << 4) + (j & 7) * 2; };
+  for (int e = tid; e < numel; e += kSmallThreads * kBatch) {
+    float x[kBatch], o[kBatch];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = min(e + i * kSmallThreads, numel - 1);
+      x[i] = to_f(gp[at]);
+      o[i] = mp ? mp[at] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int at = e + i * kSmallThreads;
+      if (at >= numel) break;
+      const int r = at / sp.cols, c = at - r * sp.cols, to = sp.flip ? place(c, r) : place(r, c);
+      const Exact u = mp ? exact_direction(x[i], o[i], p.mu, p.nesterov) : Exact{x[i], 0.f};
+      const __half h = __float2half_rn(u.u * f);
+      *reinterpret_cast<__half *>(sh.x[0][0] + to) = h;
+      *reinterpret_cast<__half *>(sh.x[1][0] + to) = rest_of(u, f, h);
+    }
+  }
+
+  Patience wait{&sh.abort, p.error, p.timeout_ns};
+  uint32_t phase = 0;
+  bool ok = true;
+  const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16);
+  constexpr int kProducts = SPLIT ? 3 : 1;
+  // A product of what all threads have written; true when its sums are in tensor memory.  Operands are boxes of 128 rows;
+  // the second one is read along its rows (inner) or across them (outer, `n` columns).
+  auto product = [&](const uint8_t *a, size_t a_part, const uint8_t *b, size_t b_part, bool b_outer, int n, int ksteps) {
+    fence_async_shared();
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if (warp == 0) {
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      if (elected()) {
+        const uint32_t idesc = 1u << 4 | (uint32_t)b_outer << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+        bool add = false;
+#pragma unroll 1
+        for (int pr = 0; pr < kProducts; ++pr) {
+          // the small products first: what an addition cuts off goes by the size of the sum so far
+          const uint32_t pa = smem_u32(a) + (SPLIT && pr == 0 ? (uint32_t)a_part : 0), pb = smem_u32(b) + (SPLIT && pr == 1 ? (uint32_t)b_part : 0);
+#pragma unroll 1
+          for (int k = 0; k < ksteps; ++k) {  // 16 inner indices; 64 to a box
+            const uint64_t da = descriptor(pa + (k >> 2) * kTall, false) + (k & 3) * desc_step(false);
+            const uint64_t db = b_outer ? (kDescBase | (uint64_t)(kTall >> 4) << 16 | (pb >> 4 & 0x3fff)) + k * desc_step(true)
+                                        : descriptor(pb + (k >> 2) * kTall, false) + (k & 3) * desc_step(false);
+            mma<1>(tmem, da, db, idesc, add);
+            add = true;
+          }
+        }
+        mma_commit<1>(smem_u32(&sh.done));
+      }
+      __syncwarp();
+    }
+    const bool good = wait.bar(smem_u32(&sh.done), phase);
+    phase ^= 1;
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    return good;
+  };
+  constexpr size_t kXPart = sizeof(sh.x[0]), kAPart = sizeof(sh.a[0]);
+  uint8_t *abox = sh.a[0][half];  // this warp's 64 columns of A and B
+  for (int it = 0; it < p.steps; ++it) {
+    const float ca = p.coef[it][0], cb = p.coef[it][1], cc = p.coef[it][2];
+    const bool last = it + 1 == p.steps;
+    if (!(ok = product(sh.x[0][0], kXPart, sh.x[0][0], kXPart, false, 128, wsteps))) break;
+    {
+      float v[64];
+      tmem_load64(lanes + half * 64, v);
+      const float t = take_out(v, row - half * 64);
+      if ((row >> 6) == half) sh.da[row] = t * kUnstore2;
+#pragma unroll
+      for (int i = 0; i < 64; ++i) v[i] *= kUnstore;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) put<SPLIT, kAPart>(abox, row, c, v + 8 * c);
+    }
+    if (!(ok = product(sh.a[0][0], kAPart, sh.a[0][0], kAPart, false, 128, nsteps))) break;
+    {
+      float v[64];
+      tmem_load64(lanes + half * 64, v);
+      const float di = sh.da[row], cs = cc * kUnstore, t = take_out(v, row - half * 64);
+      if ((row >> 6) == half) sh.db[row] = fmaf(di, fmaf(cc, di, cb), t * cc * kUnstore2);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        float o[8];
+        get<SPLIT, kAPart>(abox, row, c, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * c + i] = fmaf(fmaf(cc, di + sh.da[half * 64 + 8 * c + i], cb), o[i], v[8 * c + i] * cs);
+        put<SPLIT, kAPart>(abox, row, c, v + 8 * c);
+      }
+    }
+    if (!(ok = product(sh.a[0][0], kAPart, sh.x[0][0], kXPart, true, boxes * 64, nsteps))) break;
+    const float k = ca + sh.db[row];
+    for (int b = half; b < boxes; b += 2) {
+      float v[64];
+      __syncwarp();
+      tmem_load64(lanes + b * 64, v);
+      uint8_t *box = sh.x[0][b];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        float x[8];
+        get<true, kXPart>(box, row, c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[8 * c + i] = fmaf(k, x[i], v[8 * c + i] * kUnstore);
+        if (!last) put<true, kXPart>(box, row, c, v + 8 * c);
+      }
+      if (last) {  // as float32, columns 0 to 31 of the box where its first part was, the others where its second was
+#pragma unroll
+        for (int c = 0; c < 16; ++c)
+          *piece(box + (c >> 3) * kXPart, row, c & 7) = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
+                                                                  __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+      }
+    }
+  }
+  __syncthreads();
+  if (ok) {
+    const float scale = p.scale[sp.m0 + z / p.K] * kUnstore;
+    T *o = out + base;
+    for (int e = tid; e < numel; e += kSmallThreads) {
+      const int r = e / sp.cols, c = e - r * sp.cols, i = sp.flip ? c : r, j = sp.flip ? r : c;
+      const float v = *reinterpret_cast<const float *>(sh.x[j >> 5 & 1][j >> 6] + i * 128 + (((j >> 2 & 7) ^ (i & 7)) << 4) + (j & 3) * 4) * scale;
+      if constexpr (sizeof(T) == 4) o[e] = v;
+      else o[e] = __float2bfloat16_rn(v);
+    }
+  }
+  if (sh.abort) {  // products may be in flight: they wait for nothing, so they end within this time
+    for (int i = 0; i < 200; ++i) __nanosleep(10000);
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  if (warp == 0) tmem_free<1>(tmem, 256);
+}
+
 }  // namespace
 
 // ---------------------------------------------------------------- host side
@@ -980,6 +1206,7 @@ struct dasgd_ortho {
   int chunks = 0, rblks = 0;
   bool has_momentum = false;
   int grid = 0;
+  int small = 0;  // > 0: so many matrices, each the work of one CTA
 };
 
 namespace {
@@ -1162,6 +1389,14 @@ void coefficients(const dasgd_ortho_config *c, int &steps, float (*coef)[3]) {
 // against 214.  In float32: 809 / 811, 912 / 1105, 365 / 469, 272 / 336.
 constexpr long long kEnoughTiles = 64;
 
+// All matrices fit SMs (and no tile was asked for).  64 x 96 in float32 takes kSMALLus us instead of 77.
+bool all_small(const dasgd_ortho_config *c) {
+  if (c->tile) return false;
+  for (int i = 0; i < c->n_matrices; ++i)
+    if (std::min(c->matrices[i].rows, c->matrices[i].cols) > kSmallN || std::max(c->matrices[i].rows, c->matrices[i].cols) > kSmallW) return false;
+  return true;
+}
+
 int choose_tile(const dasgd_ortho_config *c) {
   if (c->tile) return c->tile / 128;
   long long tiles = 0;
@@ -1213,6 +1448,12 @@ void launch_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&attr)[2], int c
 
 template <typename T>
 dasgd_status run(const dasgd_ortho *op, const T *g, float *m, T *out, cudaStream_t s) {
+  if (op->small) {
+    auto kernel = k_ortho_small<sizeof(T) == 4, T>;
+    kernel<<<op->small, kSmallThreads, sizeof(SmallShared), s>>>(op->plan, g, m, out);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "ortho_step");
+  }
   const int vec = op->plan.ld % 8 == 0 && aligned(g, 16) && aligned(m, 16), vec_out = op->plan.ld % 8 == 0 && aligned(out, 16);
   k_ortho_momentum<T><<<op->chunks, kPrepThreads, 0, s>>>(op->plan, g, m, vec);
   cudaError_t e = cudaGetLastError();
@@ -1338,6 +1579,15 @@ dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, 
   op->plan = p, op->device = c.device, op->dtype = c.dtype, op->cg = cg, op->chunks = l.chunks, op->rblks = l.rblks;
   op->has_momentum = c.momentum != 0.0f;
   op->grid = (int)std::min(l.most_tiles, room) * cg;
+  if (all_small(cfg)) {
+    e = c.dtype == DASGD_F32 ? cudaFuncSetAttribute(k_ortho_small<true, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallShared))
+                             : cudaFuncSetAttribute(k_ortho_small<false, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallShared));
+    if (e != cudaSuccess) {
+      delete op;
+      return cuda_fail(e, "ortho_init");
+    }
+    op->small = (int)l.n_done;
+  }
   *out = op;
   return DASGD_OK;
 } catch (const std::bad_alloc &) {

@@ -103,6 +103,21 @@ def test_one_matrix(r, c, tile, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("kind", ["flat", "noisy", "decaying"])
+@pytest.mark.parametrize("r,c", [(1, 1), (1, 256), (256, 1), (2, 3), (8, 8), (15, 17), (63, 65), (64, 64), (65, 64), (64, 96), (100, 200), (200, 100), (127, 129), (128, 128),
+                                 (128, 256), (256, 128), (129, 127), (33, 255)])
+def test_one_small_matrix(r, c, kind, dtype):
+    check([(r, c)], dtype=dtype, kind=kind, seed=r + c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("mu,nesterov,inplace", [(0.0, False, False), (0.9, False, True), (0.95, True, False)])
+def test_many_small_matrices_in_replicas(mu, nesterov, inplace, dtype):
+    check([(64, 96), (96, 64), (128, 256), (64, 96), (7, 130), (1, 5)], K=3, dtype=dtype, gap=5, mu=mu, nesterov=nesterov, inplace=inplace,
+          scales=[1.0, 0.2, 3.0, 0.5, 1.5, 2.0], misalign=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("tile", [0, 128, 256])
 @pytest.mark.parametrize("K,shapes,gap", [(3, [(96, 200), (200, 96), (96, 200), (33, 7)], 5), (2, [(512, 512), (512, 512), (1024, 256), (256, 1024)], 8),
                                           (5, [(130, 390)], 0)])
