@@ -643,10 +643,11 @@ __device__ __forceinline__ void write_out(const Plan &p, const Tile &t, uint8_t 
 }
 
 // v[e], with a zero left in its place.  Selects, not a branch for each of 64 places: those cost 20,000 cycles.
-__device__ __forceinline__ float take_out(float (&v)[64], int e) {
+template <int N>
+__device__ __forceinline__ float take_out(float (&v)[N], int e) {
   float d = 0.f;
 #pragma unroll
-  for (int i = 0; i < 64; ++i) {
+  for (int i = 0; i < N; ++i) {
     d = i == e ? v[i] : d;
     v[i] = i == e ? 0.f : v[i];
   }
@@ -990,7 +991,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
 // kernel does momentum, norm, all steps and the result; a product waits for the one before it through a barrier of the CTA, not
 // through device memory, which takes a tile kernel 7000 cycles from product to product.  A matrix with more rows than columns is
 // held transposed.
-constexpr int kSmallN = 128, kSmallW = 256, kSmallWarps = 8, kSmallThreads = kSmallWarps * 32;
+constexpr int kSmallN = 128, kSmallW = 256, kSmallWarps = 16, kSmallThreads = kSmallWarps * 32;
 constexpr int kTall = 128 * 128;  // bytes of a box of 128 rows
 
 struct SmallShared {
@@ -1008,7 +1009,7 @@ template <bool SPLIT, typename T>
 __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const Plan p, const T *g, float *m, T *out) {
   extern __shared__ __align__(1024) uint8_t raw[];
   SmallShared &sh = *reinterpret_cast<SmallShared *>(raw);
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, q = warp & 3, unit = warp >> 2, row = q * 32 + lane;
   if (smem_u32(raw) & 1023) {  // the swizzles below need it; nothing has started yet
     if (tid == 0) atomicExch(p.error, 1);
     return;
@@ -1123,56 +1124,60 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const Plan p, 
     return good;
   };
   constexpr size_t kXPart = sizeof(sh.x[0]), kAPart = sizeof(sh.a[0]);
-  uint8_t *abox = sh.a[0][half];  // this warp's 64 columns of A and B
+  // A warp has 32 rows of the accumulators and units of 32 columns, the fourth, eighth, ... after its first; of A and B one.
+  // Rows and columns past the matrix are zero and stay so.
+  uint8_t *abox = sh.a[0][unit >> 1];
+  const int c0 = (unit & 1) * 4;  // the unit's first piece in its box
+  const bool rows = q * 32 < sp.n, square = rows && unit * 32 < sp.n, diag = unit == q;
   for (int it = 0; it < p.steps; ++it) {
     const float ca = p.coef[it][0], cb = p.coef[it][1], cc = p.coef[it][2];
     const bool last = it + 1 == p.steps;
-    if (!(ok = product(sh.x[0][0], kXPart, sh.x[0][0], kXPart, false, 128, wsteps))) break;
-    {
-      float v[64];
-      tmem_load64(lanes + half * 64, v);
-      const float t = take_out(v, row - half * 64);
-      if ((row >> 6) == half) sh.da[row] = t * kUnstore2;
+    if (!(ok = product(sh.x[0][0], kXPart, sh.x[0][0], kXPart, false, nsteps * 16, wsteps))) break;
+    if (square) {
+      float v[32];
+      tmem_load32(lanes + unit * 32, v);
+      if (diag) sh.da[row] = take_out(v, lane) * kUnstore2;
 #pragma unroll
-      for (int i = 0; i < 64; ++i) v[i] *= kUnstore;
+      for (int i = 0; i < 32; ++i) v[i] *= kUnstore;
 #pragma unroll
-      for (int c = 0; c < 8; ++c) put<SPLIT, kAPart>(abox, row, c, v + 8 * c);
+      for (int c = 0; c < 4; ++c) put<SPLIT, kAPart>(abox, row, c0 + c, v + 8 * c);
     }
-    if (!(ok = product(sh.a[0][0], kAPart, sh.a[0][0], kAPart, false, 128, nsteps))) break;
-    {
-      float v[64];
-      tmem_load64(lanes + half * 64, v);
-      const float di = sh.da[row], cs = cc * kUnstore, t = take_out(v, row - half * 64);
-      if ((row >> 6) == half) sh.db[row] = fmaf(di, fmaf(cc, di, cb), t * cc * kUnstore2);
+    if (!(ok = product(sh.a[0][0], kAPart, sh.a[0][0], kAPart, false, nsteps * 16, nsteps))) break;
+    if (square) {
+      float v[32];
+      tmem_load32(lanes + unit * 32, v);
+      const float di = sh.da[row], cs = cc * kUnstore;
+      if (diag) sh.db[row] = fmaf(di, fmaf(cc, di, cb), take_out(v, lane) * cc * kUnstore2);
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
+      for (int c = 0; c < 4; ++c) {
         float o[8];
-        get<SPLIT, kAPart>(abox, row, c, o);
+        get<SPLIT, kAPart>(abox, row, c0 + c, o);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[8 * c + i] = fmaf(fmaf(cc, di + sh.da[half * 64 + 8 * c + i], cb), o[i], v[8 * c + i] * cs);
-        put<SPLIT, kAPart>(abox, row, c, v + 8 * c);
+        for (int i = 0; i < 8; ++i) v[8 * c + i] = fmaf(fmaf(cc, di + sh.da[unit * 32 + 8 * c + i], cb), o[i], v[8 * c + i] * cs);
+        put<SPLIT, kAPart>(abox, row, c0 + c, v + 8 * c);
       }
     }
-    if (!(ok = product(sh.a[0][0], kAPart, sh.x[0][0], kXPart, true, boxes * 64, nsteps))) break;
-    const float k = ca + sh.db[row];
-    for (int b = half; b < boxes; b += 2) {
-      float v[64];
+    if (!(ok = product(sh.a[0][0], kAPart, sh.x[0][0], kXPart, true, wsteps * 16, nsteps))) break;
+    for (int u = unit; rows && u * 32 < sp.w; u += 4) {
+      const float k = ca + sh.db[row];
+      float v[32];
       __syncwarp();
-      tmem_load64(lanes + b * 64, v);
-      uint8_t *box = sh.x[0][b];
+      tmem_load32(lanes + u * 32, v);
+      uint8_t *box = sh.x[0][u >> 1];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) {
+      for (int c = 0; c < 4; ++c) {
         float x[8];
-        get<true, kXPart>(box, row, c, x);
+        get<true, kXPart>(box, row, c0 + c, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[8 * c + i] = fmaf(k, x[i], v[8 * c + i] * kUnstore);
-        if (!last) put<true, kXPart>(box, row, c, v + 8 * c);
+        if (!last) put<true, kXPart>(box, row, c0 + c, v + 8 * c);
       }
-      if (last) {  // as float32, columns 0 to 31 of the box where its first part was, the others where its second was
+      // The result in float32, where the warp's own pair was: four of the eight pieces of the unit in either part.
+      if (last) {
 #pragma unroll
-        for (int c = 0; c < 16; ++c)
-          *piece(box + (c >> 3) * kXPart, row, c & 7) = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
-                                                                  __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+        for (int c = 0; c < 8; ++c)
+          *piece(box + (c >> 2) * kXPart, row, c0 + (c & 3)) = make_uint4(__float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
+                                                                         __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
       }
     }
   }
@@ -1182,7 +1187,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const Plan p, 
     T *o = out + base;
     for (int e = tid; e < numel; e += kSmallThreads) {
       const int r = e / sp.cols, c = e - r * sp.cols, i = sp.flip ? c : r, j = sp.flip ? r : c;
-      const float v = *reinterpret_cast<const float *>(sh.x[j >> 5 & 1][j >> 6] + i * 128 + (((j >> 2 & 7) ^ (i & 7)) << 4) + (j & 3) * 4) * scale;
+      // column j: unit j / 32 of 32, in it the quadruple j / 4 % 8, four of which are in the first part, four in the second
+      const int at = (j >> 5 & 1) * 4 + (j >> 2 & 3);
+      const float v = *reinterpret_cast<const float *>(sh.x[j >> 4 & 1][j >> 6] + i * 128 + ((at ^ (i & 7)) << 4) + (j & 3) * 4) * scale;
       if constexpr (sizeof(T) == 4) o[e] = v;
       else o[e] = __float2bfloat16_rn(v);
     }
