@@ -308,11 +308,13 @@ __device__ __forceinline__ uint32_t mapped(uint32_t addr, int rank) {
   return a;
 }
 
-// arrives on the barrier at the same offset in the first CTA of the pair, or on this CTA's own
+// Arrives on the barrier at the same offset in the first CTA of the pair, or on this CTA's own.  Nothing in memory depends on
+// it (it says that accumulators have been read, which tcgen05.wait has seen to): a release to the cluster waited for all
+// of the warp's stores, 1000 to 3000 cycles.
 template <int CG>
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   if constexpr (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-  else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped(bar, 0)) : "memory");
+  else asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped(bar, 0)) : "memory");
 }
 
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
@@ -327,6 +329,16 @@ __device__ __forceinline__ unsigned load_acquire(const unsigned *p) {
   unsigned v;
   asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
   return v;
+}
+
+__device__ __forceinline__ int load_acquire_cta(const int *p) {
+  int v;
+  asm volatile("ld.acquire.cta.shared::cta.s32 %0, [%1];" : "=r"(v) : "r"(smem_u32(p)) : "memory");
+  return v;
+}
+
+__device__ __forceinline__ void store_release_cta(int *p, int v) {
+  asm volatile("st.release.cta.shared::cta.s32 [%0], %1;" ::"r"(smem_u32(p)), "r"(v) : "memory");
 }
 
 __device__ __forceinline__ void add_release(unsigned *p, unsigned v) {
@@ -507,14 +519,16 @@ __device__ __forceinline__ bool outer(const Operand &o, int kb) {  // whether th
 }
 
 constexpr int kSharedShapes = 8;  // more are read from device memory
+constexpr int kClosed = 4;        // an epilogue warp can be at most three tiles ahead of another in having its stores done
 
 struct Shared {
   uint8_t slots[kSlots][kSlotBytes];
   uint8_t stage[kEpiWarps][kStage];
   float columns[kEpiWarps][64];          // what an epilogue warp needs of the other side's diagonal
-  uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2], in[kEpiWarps];
+  uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2], in[kEpiWarps], closed[kClosed];
   Shape shapes[kSharedShapes];
   uint32_t tmem;
+  int ready;           // tiles of this CTA whose operands are known to be finished
   volatile int abort;
 };
 static_assert(sizeof(Shared) <= 227 * 1024, "shared memory of a CTA");
@@ -538,6 +552,12 @@ struct Patience {
   __device__ bool bar(uint32_t b, uint32_t parity) {
     since = 0;
     for (int i = 1; !__all_sync(0xffffffffu, mbar_try(b, parity)); ++i)
+      if ((i & 63) == 0 && __any_sync(0xffffffffu, over())) return false;
+    return true;
+  }
+  __device__ bool flag(const int *p, int want) {  // in shared memory
+    since = 0;
+    for (int i = 1; !__all_sync(0xffffffffu, load_acquire_cta(p) >= want); ++i)
       if ((i & 63) == 0 && __any_sync(0xffffffffu, over())) return false;
     return true;
   }
@@ -745,6 +765,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&sh.full[i]), 1), mbar_init(smem_u32(&sh.empty[i]), 1);
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.acc_full[i]), 1), mbar_init(smem_u32(&sh.acc_empty[i]), CG * kEpiWarps);
     for (int i = 0; i < kEpiWarps; ++i) mbar_init(smem_u32(&sh.in[i]), 1);
+    for (int i = 0; i < kClosed; ++i) mbar_init(smem_u32(&sh.closed[i]), kEpiWarps);
+    sh.ready = 0;
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -771,8 +793,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     int slot = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (int i = first; ok && walk.at(p, i, t); i += stride) {
-      if (!(ok = wait.count(p.done + t.g->z0 + t.z, needed<CG>(t)))) break;
+    for (int i = first, nt = 1; ok && walk.at(p, i, t); i += stride, ++nt) {
+      if (!(ok = wait.flag(&sh.ready, nt))) break;
       fence_async_global();
       Operand oa, ob;
       operands<CG>(t, oa, ob);
@@ -854,19 +876,44 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
         }
       }
     }
-  } else if (warp >= 4) {
+  } else if (warp == 2) {
+    // sees to it, ahead of the others, that what a tile reads has been finished by other CTAs
+    for (int i = first, nt = 1; walk.at(p, i, t); i += stride, ++nt) {
+      if (!wait.count(p.done + t.g->z0 + t.z, needed<CG>(t))) break;
+      if (lane == 0) store_release_cta(&sh.ready, nt);
+    }
+  } else if (warp == 3) {
+    // tells the other CTAs of a finished tile, when all epilogue warps have their stores done
+    for (int i = first, nt = 0; walk.at(p, i, t); i += stride, ++nt) {
+      if (!wait.bar(smem_u32(&sh.closed[nt % kClosed]), nt / kClosed & 1)) break;
+      if (lane == 0) add_release(p.done + t.g->z0 + t.z, kEpiWarps);
+    }
+  } else {
     registers<kMore, 216>();
     const int q = warp & 3, half = (warp - 4) >> 2;
     uint8_t *stage = sh.stage[warp - 4];
     float *columns = sh.columns[warp - 4];
     const uint32_t in = smem_u32(&sh.in[warp - 4]), area = smem_u32(stage);
     uint32_t in_phase = 0;
-    int n = 0;
+    int n = 0, closed = 0;  // accumulators used; tiles whose stores are done
     bool ok = true;
-    for (int i = first; ok && walk.at(p, i, t); i += stride) {
+    // The stores of a tile are waited for when the next one's loads have been asked for, and so have had time; but before this
+    // warp waits for other CTAs, which may be waiting for that tile.
+    auto settle = [&](int tiles) {
+      for (; closed < tiles; ++closed)
+        if (elected()) {
+          stores_done();
+          mbar_arrive<1>(smem_u32(&sh.closed[closed % kClosed]));
+        }
+      __syncwarp();
+    };
+    int nt = 0;
+    for (int i = first; ok && walk.at(p, i, t); i += stride, ++nt) {
       const Shape &g = *t.g;
-      // what the epilogue itself reads was finished by other CTAs: it acquires that too
-      if (!(ok = wait.count(p.done + g.z0 + t.z, needed<CG>(t)))) break;
+      if (!__all_sync(0xffffffffu, load_acquire_cta(&sh.ready) > nt)) {
+        settle(nt);
+        if (!(ok = wait.flag(&sh.ready, nt + 1))) break;
+      }
       const bool update = t.phase == UPDATE, last = update && t.it + 1 == p.steps;
       const int rows = update ? g.rows : g.n, cols = update ? g.cols : g.n;
       const int row0 = t.ti * kCols + rank * 128 + q * 32;
@@ -931,6 +978,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
         ++n;
       };
       bring(0);
+      settle(nt);
       if constexpr (SPLIT) {
         float v[CG][64];
         const int kbs = ((t.phase == GRAM ? g.w : g.n) + kBox - 1) / kBox;
@@ -965,13 +1013,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
         }
       }
       __syncwarp();
-      if (ok && elected()) {
-        stores_done();  // visible to this thread, and by the release to those that acquire
-        add_release(p.done + g.z0 + t.z, 1);
-      }
-      __syncwarp();
     }
-    if (elected()) stores_done();
+    if (ok) settle(nt);
+    else if (elected()) stores_done();
   }
   __syncwarp();
   __syncthreads();
