@@ -513,6 +513,10 @@ __device__ __forceinline__ void operands(const Tile &t, Operand &a, Operand &b) 
   else a = {xm, 0, t.ti}, b = {MAP_B, 2, t.tj};
 }
 
+// On the diagonal both sides of a symmetric product are the same rows: they are brought in once.  An SM takes in 53 to 60 bytes
+// a cycle, which is what bounds matrices of about 1024 (there two tiles in five lie on the diagonal).
+__device__ __forceinline__ bool same_sides(const Tile &t) { return t.phase != UPDATE && t.ti == t.tj; }
+
 template <int CG>
 __device__ __forceinline__ bool outer(const Operand &o, int kb) {  // whether the box of 64-wide inner block kb is read transposed
   return o.kind == 1 || (o.kind == 2 && kb / (2 * CG) < o.t);
@@ -801,6 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       const CUtensorMap *maps = p.maps + t.gi * MAPS;
       const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
       const int a0 = oa.t * kCols + rank * 128, b0 = ob.t * kCols + rank * 128;
+      const bool one = same_sides(t);
       for (int kb = 0; ok && kb < kbs; ++kb) {
         const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
         const int ax = at ? a0 : kb * kBox, ay = at ? kb * kBox : a0, bx = bt ? b0 : kb * kBox, by = bt ? kb * kBox : b0;
@@ -809,14 +814,16 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
           if (!(ok = wait.bar(smem_u32(&sh.empty[slot]), phase ^ 1))) break;
           if (elected()) {
             uint32_t full = smem_u32(&sh.full[slot]);
-            if (rank == 0) mbar_expect(full, CG * kSlotBytes);
+            if (rank == 0) mbar_expect(full, CG * (one ? kSlotBytes / 2 : kSlotBytes));
             if constexpr (CG == 2) full = mapped(full, 0);
             const uint32_t dst = slots + slot * kSlotBytes;
             const CUtensorMap *ma = maps + oa.map + part, *mb = maps + ob.map + part;
             tma_load<CG>(dst, ma, full, ax, ay, t.z);
             tma_load<CG>(dst + kBoxBytes, ma, full, at ? ax + kBox : ax, at ? ay : ay + kBox, t.z);
-            tma_load<CG>(dst + 2 * kBoxBytes, mb, full, bx, by, t.z);
-            tma_load<CG>(dst + 3 * kBoxBytes, mb, full, bt ? bx + kBox : bx, bt ? by : by + kBox, t.z);
+            if (!one) {
+              tma_load<CG>(dst + 2 * kBoxBytes, mb, full, bx, by, t.z);
+              tma_load<CG>(dst + 3 * kBoxBytes, mb, full, bt ? bx + kBox : bx, bt ? by : by + kBox, t.z);
+            }
           }
           __syncwarp();
           if (++slot == kSlots) slot = 0, phase ^= 1;
@@ -834,6 +841,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
         Operand oa, ob;
         operands<CG>(t, oa, ob);
         const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+        const bool one = same_sides(t);
         for (int kb = 0; ok && kb < kbs; ++kb) {
           const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
           const uint32_t idesc = shape | (uint32_t)at << 15 | (uint32_t)bt << 16;
@@ -852,7 +860,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
             if (!(ok = wait.bar(smem_u32(&sh.full[slot]), phase))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t src = slots + slot * kSlotBytes;
-            da[part] = descriptor(src, at), db[part] = descriptor(src + 2 * kBoxBytes, bt), used[part] = slot;
+            da[part] = descriptor(src, at), db[part] = descriptor(one ? src : src + 2 * kBoxBytes, bt), used[part] = slot;
             if (elected()) {
               if (part == 0) {
 #pragma unroll
