@@ -410,6 +410,18 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
   for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n"
+      " tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr) : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+
 __device__ __forceinline__ void tmem_load64(uint32_t addr, float (&v)[64]) {
   uint32_t r[64];
   asm volatile(
@@ -678,6 +690,12 @@ __device__ __forceinline__ float take_out(float (&v)[N], int e) {
   return d;
 }
 
+// Keeps the compiler from having several pieces in registers at once, where a thread holds 128 sums already.
+template <bool ON>
+__device__ __forceinline__ void one_by_one() {
+  if constexpr (ON) asm volatile("" ::: "memory");
+}
+
 // 64 columns of the warp's 32 rows of a finished tile, from the accumulators in v to the staging area (or to the caller's
 // array, when the step is the last).  The area holds the entries of O (square) or X (update) that belong there.
 template <bool SPLIT, typename Out>
@@ -705,13 +723,17 @@ __device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *st
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
         float o[8];
+        one_by_one<SPLIT>();
         get<SPLIT>(stage, lane, q, o);
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[8 * q + i] = fmaf(fmaf(c, di + columns[8 * q + i], b), o[i], v[8 * q + i] * cs);
       }
     }
 #pragma unroll
-    for (int q = 0; q < 8; ++q) put<SPLIT>(stage, lane, q, v + 8 * q);
+    for (int q = 0; q < 8; ++q) {
+      one_by_one<SPLIT>();
+      put<SPLIT>(stage, lane, q, v + 8 * q);
+    }
     return;
   }
   const float a = p.coef[t.it][0];
@@ -719,13 +741,17 @@ __device__ __forceinline__ void finish(const Plan &p, const Tile &t, uint8_t *st
 #pragma unroll
   for (int q = 0; q < 8; ++q) {
     float x[8];
+    one_by_one<SPLIT>();
     get<true>(stage, lane, q, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[8 * q + i] = fmaf(g.flip ? k + columns[8 * q + i] : k, x[i], v[8 * q + i] * kUnstore);
   }
   if (t.it + 1 < p.steps) {
 #pragma unroll
-    for (int q = 0; q < 8; ++q) put<true>(stage, lane, q, v + 8 * q);
+    for (int q = 0; q < 8; ++q) {
+      one_by_one<SPLIT>();
+      put<true>(stage, lane, q, v + 8 * q);
+    }
   } else {
     write_out<Out>(p, t, stage, lane, row0, col0, v, out, vec);
   }
@@ -988,26 +1014,27 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       bring(0);
       settle(nt);
       if constexpr (SPLIT) {
-        float v[CG][64];
+        float v[CG][64] = {};
         const int kbs = ((t.phase == GRAM ? g.w : g.n) + kBox - 1) / kBox;
         for (int kb = 0; kb < kbs; kb += kSum) {
           if (!(ok = accumulated())) break;
 #pragma unroll
-          for (int h = 0; h < 2 * CG; ++h) {
-            float x[32];
-            tmem_load32(lanes + (n & 1) * kCols + h * 32, x);
+          for (int h = 0; h < 4 * CG; ++h) {
+            float x[16];
+            tmem_load16(lanes + (n & 1) * kCols + h * 16, x);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              float &sum = v[h >> 1][(h & 1) * 32 + e];
-              sum = kb ? sum + x[e] : x[e];
-            }
+            for (int e = 0; e < 16; ++e) v[h >> 2][(h & 3) * 16 + e] += x[e];
           }
           release();
         }
+#pragma unroll 1
+        for (int u = 0; ok && u < CG; ++u) {  // one copy of the code, always on the first unit
+          if (u) bring(u);
+          ok = end(u, v[0]);
+          if constexpr (CG == 2) {
 #pragma unroll
-        for (int u = 0; u < CG; ++u) {
-          if (u && ok) bring(u);
-          if (ok) ok = end(u, v[u]);
+            for (int e = 0; e < 64; ++e) v[0][e] = v[1][e];
+          }
         }
       } else {
         if (!(ok = accumulated())) break;
