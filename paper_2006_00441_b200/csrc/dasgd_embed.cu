@@ -164,7 +164,7 @@ struct SortArgs {
   long long grad_stride, grad_bytes;
 };
 
-constexpr int kZeroCtas = 148 * 3;    // with the sorting clusters in front they fill the SMs
+constexpr int kZeroCtas = 148 * 4;    // with the sorting clusters in front they fill the SMs
 constexpr int kMaxCluster = 16;
 constexpr int kZeroPiece = 1 << 16;  // bytes that a CTA zeroes at a time
 
@@ -185,19 +185,15 @@ __device__ __forceinline__ void zero_piece(char *p, int n) {  // n <= kZeroPiece
 //
 // Sorting keeps a few SMs busy with latencies.  The clusters after the first K meanwhile zero the whole table of every replica
 // (rows that tokens select are written once more by the sums: cheaper than waiting to know which).
-struct SortShared {
-  uint32_t hist[kSortWarps][kMaxRadix];    // counts of the warps' digits, then where their next entry of a digit goes
-  uint32_t total[kMaxCluster][kMaxRadix];  // of every CTA of the cluster, which writes it here
-  uint32_t scan[kSortWarps];
-};
+// Shared memory of a sorting CTA, for R values of a digit: counts of the warps' digits, then where their next entry of a digit
+// goes [kSortWarps][R]; totals of every CTA of the cluster, which writes them here [kMaxCluster][R]; a scan's [kSortWarps].
+constexpr int sort_shared_bytes(int radix_bits) { return (((kSortWarps + kMaxCluster) << radix_bits) + kSortWarps) * 4; }
 
 // kBatch: entries of a lane that are loaded and voted on together; a warp whose part is no longer than that holds it in
 // registers from the counting to the placing.
 template <int kBatch>
 __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) {
-  extern __shared__ __align__(16) uint8_t sort_shared[];
-  SortShared &sh = *reinterpret_cast<SortShared *>(sort_shared);
-  auto &hist = sh.hist;
+  extern __shared__ uint32_t sort_shared[];
   asm volatile("griddepcontrol.launch_dependents;");
   cg::cluster_group cluster = cg::this_cluster();
   const int nC = cluster.num_blocks(), rank = cluster.block_rank();
@@ -212,6 +208,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
     return;
   }
   const int R = 1 << a.radix_bits;
+  uint32_t *hist = sort_shared + warp * R, *hists = sort_shared, *totals = hists + kSortWarps * R, *scan = totals + kMaxCluster * R;
   const uint32_t none = (uint32_t)a.V;
   const long long per = (a.T + nC - 1) / nC;                                   // positions of a CTA
   const long long seg = ((per + kSortWarps - 1) / kSortWarps + 31) / 32 * 32;  // positions of a warp
@@ -258,14 +255,14 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
       }
     };
     const bool single = w1 - w0 <= kBatch * 32;  // the second sweep finds everything in registers
-    for (int d = lane; d < R; d += 32) hist[warp][d] = 0;
+    for (int d = lane; d < R; d += 32) hist[d] = 0;
     __syncwarp();
     for (long long base = w0; base < w1; base += kBatch * 32) {
       load_entries(base);
       find_same(base);
 #pragma unroll
       for (int r = 0; r < kBatch; ++r) {
-        if (base + r * 32 + lane < w1 && lane == __ffs(same[r]) - 1) hist[warp][entry[r].y >> shift & (R - 1)] += __popc(same[r]);
+        if (base + r * 32 + lane < w1 && lane == __ffs(same[r]) - 1) hist[entry[r].y >> shift & (R - 1)] += __popc(same[r]);
         __syncwarp();
       }
     }
@@ -274,18 +271,18 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
       uint32_t s = 0;
 #pragma unroll
       for (int w = 0; w < kSortWarps; ++w) {
-        const uint32_t c = hist[w][tid];
-        hist[w][tid] = s;
+        const uint32_t c = hists[w * R + tid];
+        hists[w * R + tid] = s;
         s += c;
       }
-      for (int c = 0; c < nC; ++c) *cluster.map_shared_rank(&sh.total[rank][tid], c) = s;
+      for (int c = 0; c < nC; ++c) *cluster.map_shared_rank(&totals[rank * R + tid], c) = s;
     }
     cluster.sync();
     uint32_t before = 0, all = 0;
     if (tid < R) {
 #pragma unroll
       for (int c = 0; c < kMaxCluster; ++c) {
-        const uint32_t n = c < nC ? sh.total[c][tid] : 0;
+        const uint32_t n = c < nC ? totals[c * R + tid] : 0;
         all += n;
         if (c < rank) before += n;
       }
@@ -296,14 +293,14 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
       const uint32_t n = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += n;
     }
-    if (lane == 31) sh.scan[warp] = incl;
+    if (lane == 31) scan[warp] = incl;
     __syncthreads();
     uint32_t base0 = incl - all + before;
 #pragma unroll
-    for (int w = 0; w < kSortWarps; ++w) base0 += w < warp ? sh.scan[w] : 0;
+    for (int w = 0; w < kSortWarps; ++w) base0 += w < warp ? scan[w] : 0;
     if (tid < R)
 #pragma unroll
-      for (int w = 0; w < kSortWarps; ++w) hist[w][tid] += base0;
+      for (int w = 0; w < kSortWarps; ++w) hists[w * R + tid] += base0;
     __syncthreads();
     for (long long base = w0; base < w1; base += kBatch * 32) {
       if (!single) {
@@ -314,9 +311,9 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
       for (int r = 0; r < kBatch; ++r) {
         const bool in = base + r * 32 + lane < w1;
         const uint32_t d = entry[r].y >> shift & (R - 1);
-        const uint32_t at = hist[warp][d];
+        const uint32_t at = hist[d];
         __syncwarp();
-        if (in && lane == __ffs(same[r]) - 1) hist[warp][d] = at + __popc(same[r]);
+        if (in && lane == __ffs(same[r]) - 1) hist[d] = at + __popc(same[r]);
         __syncwarp();
         if (in) to[at + __popc(same[r] & ((1u << lane) - 1))] = entry[r];
       }
@@ -989,10 +986,10 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = p.cluster, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
   lc.attrs = attr, lc.numAttrs = 1;
-  lc.dynamicSmemBytes = sizeof(SortShared);
+  lc.dynamicSmemBytes = sort_shared_bytes(p.radix_bits);
   const long long rounds = (c.T + (long long)p.cluster * kSortThreads - 1) / ((long long)p.cluster * kSortThreads);
   auto kernel = rounds <= 1 ? k_sort_tokens<1> : rounds <= 2 ? k_sort_tokens<2> : rounds <= 4 ? k_sort_tokens<4> : k_sort_tokens<8>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SortShared));
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sort_shared_bytes(p.radix_bits));
   if (e == cudaSuccess && p.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&lc, kernel, so);
   if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sort");
