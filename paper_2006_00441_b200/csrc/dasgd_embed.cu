@@ -58,6 +58,17 @@ struct Raw {
 };
 
 template <typename T>
+struct Raw<T, 2> {
+  std::conditional_t<sizeof(T) == 4, uint2, uint32_t> w;
+  __device__ __forceinline__ void load(const T *p) { w = __ldg(reinterpret_cast<const decltype(w) *>(p)); }
+  __device__ __forceinline__ void clear() { w = {}; }
+  __device__ __forceinline__ void widen(float (&x)[2]) const {
+    if constexpr (sizeof(T) == 4) x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y);
+    else x[0] = __uint_as_float(w << 16), x[1] = __uint_as_float(w & 0xffff0000u);
+  }
+};
+
+template <typename T>
 struct Raw<T, 1> {
   T w;
   __device__ __forceinline__ void load(const T *p) { w = __ldg(p); }
@@ -76,6 +87,8 @@ template <int VEC>
 __device__ __forceinline__ void add_in_place(float *p, const float (&x)[VEC]) {
   if constexpr (VEC == 1) {
     asm volatile("red.relaxed.gpu.global.add.f32 [%0], %1;" ::"l"(p), "f"(x[0]) : "memory");
+  } else if constexpr (VEC == 2) {
+    asm volatile("red.relaxed.gpu.global.add.v2.f32 [%0], {%1, %2};" ::"l"(p), "f"(x[0]), "f"(x[1]) : "memory");
   } else {
 #pragma unroll
     for (int i = 0; i < VEC; i += 4)
@@ -89,6 +102,9 @@ __device__ __forceinline__ void store(T *p, const float (&x)[VEC]) {  // streami
   if constexpr (VEC == 1) {
     if constexpr (sizeof(T) == 4) *p = x[0];
     else *p = __float2bfloat16_rn(x[0]);
+  } else if constexpr (VEC == 2) {
+    if constexpr (sizeof(T) == 4) __stcs(reinterpret_cast<float2 *>(p), make_float2(x[0], x[1]));
+    else __stcs(reinterpret_cast<uint32_t *>(p), pack(x[0], x[1]));
   } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
     for (int i = 0; i < VEC / 4; ++i)
@@ -121,7 +137,7 @@ __device__ __forceinline__ long long token_at(const void *tokens, int bits, long
 // the table in flight for each thread.  Six CTAs to an SM (42 registers) matter more than rows in flight: 4 x 32768 rows of
 // 1024 bfloat16 took 74 us with four CTAs, 98 us with two and twice the rows, 85 us as a pipeline of persistent CTAs.
 template <typename W, typename O, int VEC>
-__global__ void __launch_bounds__(kThreads, 6) k_embed_lookup(const LookupArgs a) {
+__global__ void __launch_bounds__(kThreads, VEC == 8 ? 6 : 4) k_embed_lookup(const LookupArgs a) {
   constexpr int kRows = lookup_rows<W, VEC>();
   const int X = 1 << a.xs, Y = kThreads >> a.xs;
   const int tx = threadIdx.x & (X - 1), ty = threadIdx.x >> a.xs;
@@ -135,20 +151,26 @@ __global__ void __launch_bounds__(kThreads, 6) k_embed_lookup(const LookupArgs a
     const long long t = j < live ? token_at(a.tokens, a.token_bits, k * a.T + t0 + (long long)j * Y) : -1;
     tok[j] = t >= 0 && t < a.V ? (int)t : -1;
   }
-  for (int c = tx * VEC; c < a.D; c += X * VEC) {
-    Raw<W, VEC> raw[kRows];
+  constexpr int kAcross = VEC == 8 ? 1 : 4;  // units of a row that a thread has in flight
+  for (int c = tx * VEC; c < a.D; c += X * VEC * kAcross) {
+    Raw<W, VEC> raw[kAcross][kRows];
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) raw[j].load(table + (long long)max(tok[j], 0) * a.D + c);
+    for (int u = 0; u < kAcross; ++u)
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-      if (j >= live) continue;
-      if (tok[j] < 0) raw[j].clear();
-      float x[VEC];
-      raw[j].widen(x);
+      for (int j = 0; j < kRows; ++j)  // past the end the first unit again
+        raw[u][j].load(table + (long long)max(tok[j], 0) * a.D + (c + u * X * VEC < a.D ? c + u * X * VEC : c));
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) x[i] = __fmul_rn(x[i], a.scale);
-      store<O, VEC>(out + (long long)j * Y * a.D + c, x);
-    }
+    for (int u = 0; u < kAcross; ++u)
+#pragma unroll
+      for (int j = 0; j < kRows; ++j) {
+        if (j >= live || c + u * X * VEC >= a.D) continue;
+        if (tok[j] < 0) raw[u][j].clear();
+        float x[VEC];
+        raw[u][j].widen(x);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) x[i] = __fmul_rn(x[i], a.scale);
+        store<O, VEC>(out + (long long)j * Y * a.D + c + u * X * VEC, x);
+      }
   }
 }
 
@@ -338,15 +360,15 @@ struct GradArgs {
 };
 
 constexpr int kSliceCols = 256, kWideCols = 512;  // columns that a warp carries: 8 per lane, 16 where rows are aligned
-constexpr int kSumWarps = 2, kAhead = 4;
+constexpr int kSumWarps = 2;
 
-// A warp walks one block of the sorted tokens over one slice of columns, kAhead rows of dy in flight (and the rows of the
+// A warp walks one block of the sorted tokens over one slice of columns, kAhead rows of dy in flight (and bfloat16 rows of the
 // gradient that they are added to), and ends a sum wherever the token changes.  A run inside the block goes straight to
 // the gradient; one that crosses a border leaves its sum in `part`: slot 0 when it began in an earlier block, slot 1 when it
 // begins here and goes on.
 template <typename Y, typename G, int VEC, bool ADD>
 __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
-  constexpr int NV = 8 / VEC;
+  constexpr int NV = 8 / VEC, kAhead = sizeof(Y) == 2 ? 8 : 4;
   constexpr bool kOld = ADD && sizeof(G) == 2;
   const int lane = threadIdx.x & 31;
   const int s = (int)(task % a.slices);
@@ -790,9 +812,12 @@ dasgd_status cuda_fail(cudaError_t e, const char *what) {
   return dasgd_internal_fail(nullptr, DASGD_ERR_CUDA, (std::string(what) + ": " + cudaGetErrorString(e)).c_str());
 }
 
-// units of 8 elements where every row of both arrays starts on a 16-byte boundary, single elements otherwise
-bool wide(const dasgd_embed_config &c, const void *array, const void *rows) {
-  return c.D % 8 == 0 && c.ld % 8 == 0 && c.offset % 8 == 0 && aligned(array, 16) && aligned(rows, 16);
+// Elements of an access: 8 where every row of both arrays starts on a 16-byte boundary, 2 where it starts on a multiple of two
+// elements, 1 otherwise.
+int unit_of(const dasgd_embed_config &c, const void *array, const void *rows) {
+  const auto even = [&](int n) { return c.D % n == 0 && c.ld % n == 0 && c.offset % n == 0; };
+  if (even(8) && aligned(array, 16) && aligned(rows, 16)) return 8;
+  return even(2) && aligned(array, 2 * size_of(c.table_elem)) && aligned(rows, 2 * size_of(c.rows_elem)) ? 2 : 1;
 }
 
 struct Plan {  // of the gradient's workspace
@@ -861,13 +886,15 @@ Plan plan(const dasgd_embed_config &c, bool vec) {
 }
 
 template <typename W, typename O>
-void launch_lookup(const dasgd_embed_config &c, LookupArgs a, bool vec, cudaStream_t s) {
-  const int units = vec ? c.D / 8 : c.D;
-  a.xs = 0;
-  while (a.xs < 8 && (1 << a.xs) < units) ++a.xs;
-  const int rows = (kThreads >> a.xs) * (vec ? lookup_rows<W, 8>() : lookup_rows<W, 1>());
+void launch_lookup(const dasgd_embed_config &c, LookupArgs a, int vec, cudaStream_t s) {
+  // threads of a row: a power of two, as many as it has units, or a quarter where a thread takes four of them
+  const int units = c.D / vec, want = vec == 8 ? units : (units + 3) / 4;
+  a.xs = vec == 8 ? 0 : 5;
+  while (a.xs < 8 && (1 << a.xs) < want) ++a.xs;
+  const int rows = (kThreads >> a.xs) * (vec == 8 ? lookup_rows<W, 8>() : lookup_rows<W, 1>());
   const dim3 grid((unsigned)((c.T + rows - 1) / rows), (unsigned)c.K);
-  if (vec) k_embed_lookup<W, O, 8><<<grid, kThreads, 0, s>>>(a);
+  if (vec == 8) k_embed_lookup<W, O, 8><<<grid, kThreads, 0, s>>>(a);
+  else if (vec == 2) k_embed_lookup<W, O, 2><<<grid, kThreads, 0, s>>>(a);
   else k_embed_lookup<W, O, 1><<<grid, kThreads, 0, s>>>(a);
 }
 
@@ -883,11 +910,12 @@ cudaError_t launch_after(F kernel, dim3 grid, int threads, int shared, cudaStrea
 }
 
 template <typename Y, typename G>
-cudaError_t launch_sum(const GradArgs &a, bool vec, long long ctas, cudaStream_t s) {
+cudaError_t launch_sum(const GradArgs &a, int vec, long long ctas, cudaStream_t s) {
   const dim3 grid((unsigned)ctas);
   auto launch = [&](auto add) -> cudaError_t {
     constexpr bool kAdd = decltype(add)::value;
-    if (!vec) return launch_after(k_embed_sum<Y, G, 1, kAdd>, grid, kSumWarps * 32, 0, s, a);
+    if (vec == 1) return launch_after(k_embed_sum<Y, G, 1, kAdd>, grid, kSumWarps * 32, 0, s, a);
+    if (vec == 2) return launch_after(k_embed_sum<Y, G, 2, kAdd>, grid, kSumWarps * 32, 0, s, a);
     constexpr int kShared = kSumWarps * Ring<Y, G, kAdd>::kBytes;
     if (kShared > 48 * 1024) {
       const cudaError_t e = cudaFuncSetAttribute(k_embed_sum<Y, G, 8, kAdd>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
@@ -925,7 +953,7 @@ dasgd_status dasgd_embed_lookup(const dasgd_embed_config *cfg, const void *table
   a.tokens = tokens;
   a.out = out;
   a.ld = c.ld, a.T = c.T, a.V = c.V, a.D = c.D, a.token_bits = c.token_bits, a.scale = c.scale;
-  const bool vec = wide(c, table_array, out);
+  const int vec = unit_of(c, table_array, out);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (c.table_elem == DASGD_ELEM_F32) {
     if (c.rows_elem == DASGD_ELEM_F32) launch_lookup<float, float>(c, a, vec, s);
@@ -951,8 +979,8 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   dasgd_status st = check(cfg, "embed_gradient");
   if (st != DASGD_OK) return st;
   const dasgd_embed_config &c = *cfg;
-  const bool vec = wide(c, grad_array, dy);
-  const Plan p = plan(c, vec);
+  const int vec = unit_of(c, grad_array, dy);
+  const Plan p = plan(c, vec == 8);
   if (c.T == 0 && c.accumulate) return DASGD_OK;
   if (!grad_array || (c.T && (!dy || !tokens))) return bad("embed_gradient: dy, tokens and grad_array must not be NULL");
   if (!workspace || !aligned(workspace, 256) || workspace_bytes < (int64_t)p.bytes)
@@ -1009,7 +1037,7 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   else e = launch_sum<__nv_bfloat16, __nv_bfloat16>(a, vec, sum_ctas, s);
   if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sums");
   if (p.blocks > 1) {
-    e = g32 ? launch_join<float>(a, vec, s) : launch_join<__nv_bfloat16>(a, vec, s);
+    e = g32 ? launch_join<float>(a, vec == 8, s) : launch_join<__nv_bfloat16>(a, vec == 8, s);
     if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: joining");
   }
   e = cudaGetLastError();

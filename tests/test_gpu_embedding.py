@@ -37,7 +37,8 @@ def valid(t, V):
 @pytest.mark.parametrize("wt", ["f32", "bf16"])
 @pytest.mark.parametrize("ot", ["f32", "bf16"])
 @pytest.mark.parametrize("K,T,V,D,gap,it", [(1, 1, 1, 1, 0, torch.int64), (3, 1, 100, 1024, 0, torch.int32), (2, 77, 513, 333, 5, torch.int64),
-                                            (2, 500, 64, 8, 8, torch.int32), (1, 1000, 1000, 2056, 16, torch.int64), (4, 0, 10, 16, 0, torch.int64)])
+                                            (2, 500, 64, 8, 8, torch.int32), (1, 1000, 1000, 2056, 16, torch.int64), (4, 0, 10, 16, 0, torch.int64),
+                                            (3, 333, 70, 1002, 2, torch.int64), (2, 129, 33, 6, 4, torch.int32), (2, 50, 20, 130, 0, torch.int64)])
 def test_lookup(K, T, V, D, gap, it, wt, ot):
     from paper_2006_00441_b200 import binding as B
     gen, tok, ld = make(K, T, V, D, gap, it=it)
@@ -90,6 +91,7 @@ CASES = [
     (2, 31, 7, 8, 8, "zipf", torch.int64, 0.1), (2, 33, 1000, 333, 5, "zipf", torch.int32, 0.1), (1, 1024, 300, 64, 0, "uniform", torch.int64, 0.5),
     (1, 1025, 300, 72, 0, "same", torch.int64, 0.0), (2, 2049, 70000, 40, 16, "zipf", torch.int64, 0.1), (2, 5000, 259, 264, 0, "zipf", torch.int32, 0.0),
     (1, 9001, 3, 1024, 0, "uniform", torch.int64, 0.1), (1, 70001, 5003, 16, 0, "zipf", torch.int64, 0.05), (2, 777, 100, 32, 0, "none", torch.int64, 0.0),
+    (2, 700, 90, 334, 4, "zipf", torch.int64, 0.1), (3, 1500, 40, 12, 2, "zipf", torch.int32, 0.0), (1, 600, 30, 1002, 0, "uniform", torch.int64, 0.2),
     (5, 640, 511, 520, 8, "zipf", torch.int64, 0.1), (1, 12000, 512, 1032, 0, "same", torch.int32, 0.3), (1, 300, 300000, 8, 0, "uniform", torch.int64, 0.0),
 ]
 
