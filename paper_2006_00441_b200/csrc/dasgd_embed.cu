@@ -26,7 +26,7 @@ extern "C" __attribute__((visibility("hidden"))) dasgd_status dasgd_internal_fai
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kMaxRadixBits = 9, kMaxRadix = 1 << kMaxRadixBits;
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kMaxRadixBits = 9;
 
 // ---------------------------------------------------------------- loads and stores of VEC elements
 

@@ -1475,7 +1475,7 @@ void coefficients(const dasgd_ortho_config *c, int &steps, float (*coef)[3]) {
 // against 214.  In float32: 809 / 811, 912 / 1105, 365 / 469, 272 / 336.
 constexpr long long kEnoughTiles = 64;
 
-// All matrices fit SMs (and no tile was asked for).  64 x 96 in float32 takes kSMALLus us instead of 77.
+// All matrices fit SMs (and no tile was asked for).  64 x 96 in float32 takes 30 us instead of 77.
 bool all_small(const dasgd_ortho_config *c) {
   if (c->tile) return false;
   for (int i = 0; i < c->n_matrices; ++i)
