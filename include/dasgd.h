@@ -395,6 +395,7 @@ typedef struct {
   int32_t steps;               /* 1 .. 16; 0 = 5                                                                  */
   int32_t nesterov, device;
   int32_t tile;                /* 0 = by size; 128 or 256: side of the tiles that the products are computed in    */
+  int32_t split;               /* 0 = by size; with tile 128: 1, 2 or 4 CTAs share the inner dimension of a tile     */
   uint32_t timeout_ms;         /* limit of every wait inside the kernel; 0 = 10000                                */
   int64_t ld;                  /* row stride of g, m and out, elements                                            */
   float momentum, eps;

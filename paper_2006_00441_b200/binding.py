@@ -77,7 +77,7 @@ class dasgd_matrix(ctypes.Structure):
 class dasgd_ortho_config(ctypes.Structure):
     _fields_ = [
         ("K", ctypes.c_int32), ("n_matrices", ctypes.c_int32), ("dtype", ctypes.c_int32), ("steps", ctypes.c_int32),
-        ("nesterov", ctypes.c_int32), ("device", ctypes.c_int32), ("tile", ctypes.c_int32), ("timeout_ms", ctypes.c_uint32),
+        ("nesterov", ctypes.c_int32), ("device", ctypes.c_int32), ("tile", ctypes.c_int32), ("split", ctypes.c_int32), ("timeout_ms", ctypes.c_uint32),
         ("ld", ctypes.c_int64), ("momentum", ctypes.c_float), ("eps", ctypes.c_float),
         ("matrices", ctypes.POINTER(dasgd_matrix)), ("coefficients", ctypes.POINTER(ctypes.c_float)),
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_int64),
@@ -480,7 +480,7 @@ class Ortho:
     """
 
     def __init__(self, K, ld, matrices, dtype=DASGD_F32, momentum=0.95, nesterov=True, steps=5, coefficients=None, eps=1e-7,
-                 device=0, tile=0, timeout_ms=0):
+                 device=0, tile=0, split=0, timeout_ms=0):
         if not torch.cuda.is_available():
             raise RuntimeError("Ortho needs a CUDA device; there is no CPU implementation")
         self.op = None
@@ -489,7 +489,8 @@ class Ortho:
         self.gdtype = torch.bfloat16 if dtype == DASGD_BF16_MASTER_F32 else torch.float32
         c = dasgd_ortho_config()
         c.K, c.n_matrices, c.dtype, c.steps, c.device, c.ld = K, len(matrices), dtype, steps, device, ld
-        c.momentum, c.nesterov, c.eps, c.tile, c.timeout_ms = momentum, int(nesterov and momentum != 0), eps, tile, timeout_ms
+        c.momentum, c.nesterov, c.eps = momentum, int(nesterov and momentum != 0), eps
+        c.tile, c.split, c.timeout_ms = tile, split, timeout_ms
         c.matrices = (dasgd_matrix * len(matrices))(*(dasgd_matrix(*m, *((1.0,) if len(m) == 3 else ())) for m in matrices))
         if coefficients is not None:
             flat = list(coefficients)

@@ -325,6 +325,22 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
   return ok;
 }
 
+__device__ __forceinline__ bool mbar_try_cluster(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+      : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+
+__device__ __forceinline__ void mbar_arrive_release(uint32_t bar, int rank) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(mapped(bar, rank)) : "memory");
+}
+
+__device__ __forceinline__ void store_remote(uint32_t addr, float a, float b, float c, float d) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(a), "f"(b), "f"(c), "f"(d) : "memory");
+}
+
 __device__ __forceinline__ unsigned load_acquire(const unsigned *p) {
   unsigned v;
   asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
@@ -542,6 +558,7 @@ struct Shared {
   uint8_t stage[kEpiWarps][kStage];
   float columns[kEpiWarps][64];          // what an epilogue warp needs of the other side's diagonal
   uint64_t full[kSlots], empty[kSlots], acc_full[2], acc_empty[2], in[kEpiWarps], closed[kClosed];
+  uint64_t part_in[kEpiWarps], part_out[kEpiWarps];  // partial sums that have arrived; that may be sent again
   Shape shapes[kSharedShapes];
   uint32_t tmem;
   int ready;           // tiles of this CTA whose operands are known to be finished
@@ -568,6 +585,12 @@ struct Patience {
   __device__ bool bar(uint32_t b, uint32_t parity) {
     since = 0;
     for (int i = 1; !__all_sync(0xffffffffu, mbar_try(b, parity)); ++i)
+      if ((i & 63) == 0 && __any_sync(0xffffffffu, over())) return false;
+    return true;
+  }
+  __device__ bool bar_cluster(uint32_t b, uint32_t parity) {
+    since = 0;
+    for (int i = 1; !__all_sync(0xffffffffu, mbar_try_cluster(b, parity)); ++i)
       if ((i & 63) == 0 && __any_sync(0xffffffffu, over())) return false;
     return true;
   }
@@ -776,11 +799,16 @@ __device__ __forceinline__ void registers() {
 // CG CTAs work on a tile of 128 CG x 128 CG.  Warp 0 loads, warp 1 multiplies, warps 4 to 11 finish tiles; two accumulators
 // in tensor memory let the next tile's products run while a tile is finished.  CTA (or pair) q takes tiles q, q + Q, ...:
 // every CTA is resident (cooperative launch) and tiles depend only on earlier ones, so the wait for them ends.
-template <int CG, bool SPLIT, typename Out>
+//
+// With SK > 1 (and CG = 1) a cluster of SK CTAs shares a tile: each sums a part of the inner dimension, then sends the
+// rows that are not its own quarter (or half) of the tile to the CTAs that finish them, through distributed shared memory into
+// the staging areas of warps that finish nothing there.  Partial sums are added in the order of the CTAs.
+template <int CG, int SK, bool SPLIT, typename Out>
 __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *out, int vec) {
   extern __shared__ __align__(1024) uint8_t raw[];
   Shared &sh = *reinterpret_cast<Shared *>(raw);
-  constexpr int kCols = 128 * CG;
+  static_assert(CG == 1 || SK == 1, "pairs of CTAs do not share tiles further");
+  constexpr int kCols = 128 * CG, kOwners = kEpiWarps / SK, kQuarters = 4 / SK;  // epilogue warps that finish; quarters of the rows
   const uint32_t slots = smem_u32(sh.slots);
   if (slots & 1023) {  // the swizzles below need it; nothing has started yet
     if (threadIdx.x == 0) atomicExch(p.error, 1);
@@ -788,14 +816,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int rank = 0;
+  int share = 0;
   if constexpr (CG == 2) asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(rank));
-  const int first = blockIdx.x / CG, stride = gridDim.x / CG;
+  if constexpr (SK > 1) asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(share));
+  const int first = blockIdx.x / (CG * SK), stride = gridDim.x / (CG * SK);
+  auto blocks = [&](const Tile &t, int &k0, int &k1) {  // this CTA's part of the inner dimension
+    const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+    k0 = kbs * share / SK, k1 = kbs * (share + 1) / SK;
+  };
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&sh.full[i]), 1), mbar_init(smem_u32(&sh.empty[i]), 1);
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.acc_full[i]), 1), mbar_init(smem_u32(&sh.acc_empty[i]), CG * kEpiWarps);
     for (int i = 0; i < kEpiWarps; ++i) mbar_init(smem_u32(&sh.in[i]), 1);
-    for (int i = 0; i < kClosed; ++i) mbar_init(smem_u32(&sh.closed[i]), kEpiWarps);
+    for (int i = 0; i < kClosed; ++i) mbar_init(smem_u32(&sh.closed[i]), kOwners);
+    if constexpr (SK > 1)
+      for (int i = 0; i < kEpiWarps; ++i) mbar_init(smem_u32(&sh.part_in[i]), SK - 1), mbar_init(smem_u32(&sh.part_out[i]), 1);
     sh.ready = 0;
     sh.abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -809,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   if (warp == 2) tmem_alloc<CG>(smem_u32(&sh.tmem), 2 * kCols);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if constexpr (CG == 2) cluster_barrier();
+  if constexpr (CG * SK > 1) cluster_barrier();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = sh.tmem;
   Patience wait{&sh.abort, p.error, p.timeout_ns};
@@ -829,10 +865,11 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       Operand oa, ob;
       operands<CG>(t, oa, ob);
       const CUtensorMap *maps = p.maps + t.gi * MAPS;
-      const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+      int k0, k1;
+      blocks(t, k0, k1);
       const int a0 = oa.t * kCols + rank * 128, b0 = ob.t * kCols + rank * 128;
       const bool one = same_sides(t);
-      for (int kb = 0; ok && kb < kbs; ++kb) {
+      for (int kb = k0; ok && kb < k1; ++kb) {
         const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
         const int ax = at ? a0 : kb * kBox, ay = at ? kb * kBox : a0, bx = bt ? b0 : kb * kBox, by = bt ? kb * kBox : b0;
 #pragma unroll
@@ -866,9 +903,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
       for (int i = first; ok && walk.at(p, i, t); i += stride) {
         Operand oa, ob;
         operands<CG>(t, oa, ob);
-        const int kbs = ((t.phase == GRAM ? t.g->w : t.g->n) + kBox - 1) / kBox;
+        int k0, k1;
+        blocks(t, k0, k1);
         const bool one = same_sides(t);
-        for (int kb = 0; ok && kb < kbs; ++kb) {
+        for (int kb = k0; ok && kb < k1; ++kb) {
           const bool at = outer<CG>(oa, kb), bt = outer<CG>(ob, kb);
           const uint32_t idesc = shape | (uint32_t)at << 15 | (uint32_t)bt << 16;
           const uint64_t sa = desc_step(at), sb = desc_step(bt);
@@ -876,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
           int used[kParts];
           const int acc = n & 1;
           const uint32_t d = tmem + acc * kCols;
-          const bool fresh = kb % kSum == 0, full = kb == kbs - 1 || kb % kSum == kSum - 1;
+          const bool fresh = (kb - k0) % kSum == 0, full = kb == k1 - 1 || (kb - k0) % kSum == kSum - 1;
           if (fresh) {
             if (!(ok = wait.bar(smem_u32(&sh.acc_empty[acc]), (n >> 1 & 1) ^ 1))) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -920,7 +958,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     // tells the other CTAs of a finished tile, when all epilogue warps have their stores done
     for (int i = first, nt = 0; walk.at(p, i, t); i += stride, ++nt) {
       if (!wait.bar(smem_u32(&sh.closed[nt % kClosed]), nt / kClosed & 1)) break;
-      if (lane == 0) add_release(p.done + t.g->z0 + t.z, kEpiWarps);
+      if (lane == 0) add_release(p.done + t.g->z0 + t.z, kOwners);
     }
   } else {
     registers<kMore, 216>();
@@ -930,11 +968,12 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
     const uint32_t in = smem_u32(&sh.in[warp - 4]), area = smem_u32(stage);
     uint32_t in_phase = 0;
     int n = 0, closed = 0;  // accumulators used; tiles whose stores are done
+    const bool owner = SK == 1 || q / kQuarters == share;  // finishes its rows; else sends its sums to the CTA that does
     bool ok = true;
     // The stores of a tile are waited for when the next one's loads have been asked for, and so have had time; but before this
     // warp waits for other CTAs, which may be waiting for that tile.
     auto settle = [&](int tiles) {
-      for (; closed < tiles; ++closed)
+      for (; owner && closed < tiles; ++closed)
         if (elected()) {
           stores_done();
           mbar_arrive<1>(smem_u32(&sh.closed[closed % kClosed]));
@@ -1011,12 +1050,50 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
         if (elected()) mbar_arrive<CG>(smem_u32(&sh.acc_empty[n & 1]));
         ++n;
       };
-      bring(0);
+      // Sums of other CTAs: true when v is complete and this warp is to finish it.
+      auto gather = [&](float (&v)[64]) {
+        if constexpr (SK > 1) {
+          const int w = warp - 4, quarter = q % kQuarters;
+          if (!owner) {
+            const int to = q / kQuarters;
+            if (nt && !(ok = wait.bar_cluster(smem_u32(&sh.part_out[w]), nt - 1 & 1))) return false;
+            const uint32_t area = mapped(smem_u32(sh.stage[half * 4 + share * kQuarters + quarter]), to) + lane * 16;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) store_remote(area + c * 512, v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+            __syncwarp();
+            if (elected()) mbar_arrive_release(smem_u32(&sh.part_in[w]), to);
+            return false;
+          }
+          if (!(ok = wait.bar_cluster(smem_u32(&sh.part_in[w]), nt & 1))) return false;
+#pragma unroll 1
+          for (int s = 0; s < SK; ++s) {
+            if (s == share) continue;
+            const uint8_t *area = sh.stage[half * 4 + s * kQuarters + quarter] + lane * 16;
+#pragma unroll
+            for (int c = 0; c < 16; ++c) {
+              const float4 x = *reinterpret_cast<const float4 *>(area + c * 512);
+              v[4 * c] += x.x, v[4 * c + 1] += x.y, v[4 * c + 2] += x.z, v[4 * c + 3] += x.w;
+            }
+          }
+        }
+        return true;
+      };
+      // The area may be sent to again.
+      auto make_room = [&]() {
+        if constexpr (SK > 1) {
+          __syncwarp();
+          if (elected())
+            for (int s = 0; s < SK; ++s)
+              if (s != share) mbar_arrive_release(smem_u32(&sh.part_out[warp - 4]), s);
+        }
+      };
+      if (owner) bring(0);
       settle(nt);
+      int k0, k1;
+      blocks(t, k0, k1);
       if constexpr (SPLIT) {
         float v[CG][64] = {};
-        const int kbs = ((t.phase == GRAM ? g.w : g.n) + kBox - 1) / kBox;
-        for (int kb = 0; kb < kbs; kb += kSum) {
+        for (int kb = k0; kb < k1; kb += kSum) {
           if (!(ok = accumulated())) break;
 #pragma unroll
           for (int h = 0; h < 4 * CG; ++h) {
@@ -1027,6 +1104,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
           }
           release();
         }
+        if (!ok || !gather(v[0])) continue;
 #pragma unroll 1
         for (int u = 0; ok && u < CG; ++u) {  // one copy of the code, always on the first unit
           if (u) bring(u);
@@ -1036,15 +1114,22 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
             for (int e = 0; e < 64; ++e) v[0][e] = v[1][e];
           }
         }
+        if (ok) make_room();
       } else {
-        if (!(ok = accumulated())) break;
+        const bool some = SK == 1 || k0 < k1;
+        if (some && !(ok = accumulated())) break;
 #pragma unroll 1
         for (int u = 0; ok && u < CG; ++u) {
           if (u) bring(u);
-          float v[64];
-          tmem_load64(lanes + (n & 1) * kCols + u * 64, v);
-          if (u == CG - 1) release();
-          ok = end(u, v);
+          float v[64] = {};
+          if (some) {
+            tmem_load64(lanes + (n & 1) * kCols + u * 64, v);
+            if (u == CG - 1) release();
+          }
+          if (gather(v)) {
+            ok = end(u, v);
+            if (ok) make_room();
+          }
         }
       }
       __syncwarp();
@@ -1059,7 +1144,7 @@ __global__ void __launch_bounds__(kThreads, 1) k_ortho_steps(const Plan p, Out *
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  if constexpr (CG == 2) cluster_barrier();
+  if constexpr (CG * SK > 1) cluster_barrier();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 2) tmem_free<CG>(tmem, 2 * kCols);
 }
@@ -1288,7 +1373,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const Plan p, 
 
 struct dasgd_ortho {
   Plan plan{};
-  int device = 0, dtype = 0, cg = 1;
+  int device = 0, dtype = 0, cg = 1, sk = 1;  // CTAs of a tile side by side; that share a tile's inner dimension
   int chunks = 0, rblks = 0;
   bool has_momentum = false;
   int grid = 0;
@@ -1445,6 +1530,7 @@ dasgd_status check(const dasgd_ortho_config *c, const char *who) {
   if (c->nesterov && c->momentum == 0.0f) return bad(at + "nesterov needs momentum > 0");
   if (!(c->eps >= 0.0f && isfinite(c->eps))) return bad(at + "eps must be >= 0");
   if (c->tile != 0 && c->tile != 128 && c->tile != 256) return bad(at + "tile must be 0, 128 or 256");
+  if (c->split != 0 && !(c->tile == 128 && (c->split == 1 || c->split == 2 || c->split == 4))) return bad(at + "split must be 0, or 1, 2 or 4 with tile 128");
   if (c->device < 0) return bad(at + "device must be >= 0");
   std::vector<std::pair<int64_t, int64_t>> spans;
   for (int i = 0; i < c->n_matrices; ++i) {
@@ -1491,6 +1577,21 @@ int choose_tile(const dasgd_ortho_config *c) {
   return tiles * c->K >= kEnoughTiles ? 2 : 1;
 }
 
+// CTAs that share a tile's inner dimension, where the tiles of a product leave SMs idle (the caller halves it until all tiles are
+// resident at once).  A 64-wide block of the inner dimension takes a CTA 620 cycles, or 1190 where operands are pairs; handing
+// partial sums over costs a product 2500 cycles between two CTAs and 6400 between four.  The longest of the matrices has
+// (w + 2 n) / 64 blocks in a step's three products.  One CTA, two, four (us): float32 256^2 124, 131, 152; 300 x 600 157, 154, 166;
+// 768^2 217, 187; 1024^2 269, 220; 100 x 4000 328, 239, 206.  bfloat16 768^2 142, 148; 1024^2 172, 167; 100 x 4000 199, 174, 169.
+int choose_split(const dasgd_ortho_config *c) {
+  int blocks = 0;
+  for (int i = 0; i < c->n_matrices; ++i) {
+    const dasgd_matrix &m = c->matrices[i];
+    blocks = std::max(blocks, (std::max(m.rows, m.cols) + 2 * std::min(m.rows, m.cols)) / kBox);
+  }
+  if (c->dtype == DASGD_F32) return blocks >= 40 ? 4 : blocks >= 18 ? 2 : 1;
+  return blocks >= 60 ? 4 : blocks >= 48 ? 2 : 1;
+}
+
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
@@ -1516,20 +1617,25 @@ bool encode(EncodeTiled enc, CUtensorMap *map, void *base, int rows, int cols, i
   return encode_box(enc, map, base, rows, cols, ld, batch, kBox) && encode_box(enc, map + MAP_EPI, base, rows, cols, ld, batch, kStageRows);
 }
 
-template <typename F>
-dasgd_status with_kernel(int cg, int dtype, F f) {
-  if (dtype == DASGD_F32) return cg == 1 ? f(k_ortho_steps<1, true, float>, (float *)nullptr) : f(k_ortho_steps<2, true, float>, (float *)nullptr);
-  return cg == 1 ? f(k_ortho_steps<1, false, __nv_bfloat16>, (__nv_bfloat16 *)nullptr)
-                 : f(k_ortho_steps<2, false, __nv_bfloat16>, (__nv_bfloat16 *)nullptr);
+template <typename T, typename F>
+dasgd_status with_kernel_of(int cg, int sk, F f) {
+  constexpr bool kPairs = sizeof(T) == 4;
+  if (cg == 2) return f(k_ortho_steps<2, 1, kPairs, T>, (T *)nullptr);
+  return sk == 4 ? f(k_ortho_steps<1, 4, kPairs, T>, (T *)nullptr) : sk == 2 ? f(k_ortho_steps<1, 2, kPairs, T>, (T *)nullptr) : f(k_ortho_steps<1, 1, kPairs, T>, (T *)nullptr);
 }
 
-void launch_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&attr)[2], int cg, int grid, cudaStream_t s) {
+template <typename F>
+dasgd_status with_kernel(int cg, int sk, int dtype, F f) {
+  return dtype == DASGD_F32 ? with_kernel_of<float>(cg, sk, f) : with_kernel_of<__nv_bfloat16>(cg, sk, f);
+}
+
+void launch_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&attr)[2], int ctas, int grid, cudaStream_t s) {
   lc = cudaLaunchConfig_t{};
   lc.gridDim = dim3(grid), lc.blockDim = dim3(kThreads), lc.dynamicSmemBytes = (int)sizeof(Shared), lc.stream = s;
   attr[0].id = cudaLaunchAttributeCooperative, attr[0].val.cooperative = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = cg, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
-  lc.attrs = attr, lc.numAttrs = cg == 1 ? 1 : 2;
+  attr[1].val.clusterDim.x = ctas, attr[1].val.clusterDim.y = 1, attr[1].val.clusterDim.z = 1;
+  lc.attrs = attr, lc.numAttrs = ctas == 1 ? 1 : 2;
 }
 
 template <typename T>
@@ -1551,12 +1657,12 @@ dasgd_status run(const dasgd_ortho *op, const T *g, float *m, T *out, cudaStream
   scale.gridDim = dim3(op->rblks), scale.blockDim = dim3(kPrepThreads), scale.stream = s, scale.attrs = after, scale.numAttrs = 1;
   if ((e = cudaLaunchKernelEx(&scale, k_ortho_scale<T>, op->plan, g, static_cast<const float *>(m), vec)) != cudaSuccess)
     return cuda_fail(e, "ortho_step");
-  return with_kernel(op->cg, op->dtype, [&](auto kernel, auto *type) -> dasgd_status {
+  return with_kernel(op->cg, op->sk, op->dtype, [&](auto kernel, auto *type) -> dasgd_status {
     using Out = std::remove_pointer_t<decltype(type)>;
     if constexpr (std::is_same_v<Out, T>) {
       cudaLaunchConfig_t lc;
       cudaLaunchAttribute attr[2];
-      launch_config(lc, attr, op->cg, op->grid, s);
+      launch_config(lc, attr, op->cg * op->sk, op->grid, s);
       const cudaError_t err = cudaLaunchKernelEx(&lc, kernel, op->plan, out, vec_out);
       return err == cudaSuccess ? DASGD_OK : cuda_fail(err, "ortho_step");
     }
@@ -1646,25 +1752,31 @@ dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, 
   p.mu = c.momentum, p.eps = c.eps, p.nesterov = c.nesterov != 0;
   p.timeout_ns = (c.timeout_ms ? c.timeout_ms : 10000u) * 1000000ull;
 
-  int sms = 0, clusters = 0;
-  st = with_kernel(cg, c.dtype, [&](auto kernel, auto *) -> dasgd_status {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c.device);
-    if (e == cudaSuccess && cg == 2) {
-      cudaLaunchConfig_t lc;
-      cudaLaunchAttribute attr[2];
-      launch_config(lc, attr, cg, sms / 2 * 2, s);
-      e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
-    }
-    return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "ortho_init");
-  });
-  if (st != DASGD_OK) return st;
-  const long long room = cg == 2 ? std::min(clusters, sms / 2) : sms;
+  // CTAs that may share a tile: as many as leave all tiles of a product resident at once
+  int sms = 0, sk = c.split ? c.split : cg == 1 ? choose_split(cfg) : 1;
+  if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c.device)) != cudaSuccess) return cuda_fail(e, "ortho_init");
+  long long room = 0;
+  for (;; sk /= 2) {
+    int clusters = 0;
+    st = with_kernel(cg, sk, c.dtype, [&](auto kernel, auto *) -> dasgd_status {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+      if (e == cudaSuccess && cg * sk > 1) {
+        cudaLaunchConfig_t lc;
+        cudaLaunchAttribute attr[2];
+        launch_config(lc, attr, cg * sk, sms / (cg * sk) * (cg * sk), s);
+        e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
+      }
+      return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "ortho_init");
+    });
+    if (st != DASGD_OK) return st;
+    room = cg * sk > 1 ? std::min(clusters, sms / (cg * sk)) : sms;
+    if (c.split || sk == 1 || room >= l.most_tiles) break;
+  }
   if (room < 1) return unsupported("ortho_init: the kernel does not fit this GPU");
   dasgd_ortho *op = new dasgd_ortho;
-  op->plan = p, op->device = c.device, op->dtype = c.dtype, op->cg = cg, op->chunks = l.chunks, op->rblks = l.rblks;
+  op->plan = p, op->device = c.device, op->dtype = c.dtype, op->cg = cg, op->sk = sk, op->chunks = l.chunks, op->rblks = l.rblks;
   op->has_momentum = c.momentum != 0.0f;
-  op->grid = (int)std::min(l.most_tiles, room) * cg;
+  op->grid = (int)std::min(l.most_tiles, room) * cg * sk;
   if (all_small(cfg)) {
     e = c.dtype == DASGD_F32 ? cudaFuncSetAttribute(k_ortho_small<true, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallShared))
                              : cudaFuncSetAttribute(k_ortho_small<false, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallShared));

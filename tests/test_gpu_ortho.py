@@ -45,7 +45,7 @@ def sample(gen, r, c, kind):
     return low + {"noisy": 0.1, "decaying": 0.01}[kind] * x
 
 
-def check(shapes, K=1, dtype=F32, gap=0, mu=0.95, nesterov=True, steps=5, coef=None, tile=0, kind="noisy", seed=0, inplace=False, misalign=0, scales=None):
+def check(shapes, K=1, dtype=F32, gap=0, mu=0.95, nesterov=True, steps=5, coef=None, tile=0, split=0, kind="noisy", seed=0, inplace=False, misalign=0, scales=None):
     from paper_2006_00441_b200 import binding as B
     gen = torch.Generator("cuda").manual_seed(seed)
     places, at = [], gap
@@ -65,7 +65,7 @@ def check(shapes, K=1, dtype=F32, gap=0, mu=0.95, nesterov=True, steps=5, coef=N
             g[k, o:o + r * c] = (1e-3 * sample(gen, r, c, kind)).reshape(-1).to(gd)
             m[k, o:o + r * c] = (5e-3 * sample(gen, r, c, kind)).reshape(-1)
     g0, m0 = g.clone(), m.clone()
-    op = B.Ortho(K, ld, places, dtype=dtype, momentum=mu, nesterov=nesterov, steps=steps, coefficients=coef, tile=tile)
+    op = B.Ortho(K, ld, places, dtype=dtype, momentum=mu, nesterov=nesterov, steps=steps, coefficients=coef, tile=tile, split=split)
     got = op.step(g, m if mu else None, out=None if inplace else out)
     op.sync()
     covered = torch.zeros(ld, dtype=torch.bool, device="cuda")
@@ -100,6 +100,14 @@ def check(shapes, K=1, dtype=F32, gap=0, mu=0.95, nesterov=True, steps=5, coef=N
                                  (100, 1000), (1000, 100), (511, 640), (640, 511)])
 def test_one_matrix(r, c, tile, dtype):
     check([(r, c)], dtype=dtype, tile=tile, seed=r + c)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("split", [2, 4])
+@pytest.mark.parametrize("shapes,K", [([(1, 1)], 1), ([(64, 64)], 1), ([(65, 130)], 1), ([(300, 190)], 1), ([(333, 1000), (1001, 77), (129, 129)], 3), ([(700, 700)], 1),
+                                      ([(1000, 260), (260, 1000), (128, 64)], 2), ([(1024, 1024)] * 3, 2)])
+def test_tiles_whose_inner_dimension_is_shared(shapes, K, split, dtype):
+    check(shapes, K=K, dtype=dtype, tile=128, split=split, gap=3)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])

@@ -70,7 +70,7 @@ def _ortho(matrices=((0, 8, 8),), **kw):
 @pytest.mark.parametrize("bad,frag", [
     (dict(K=0), "K must"), (dict(dtype=5), "dtype"), (dict(n_matrices=0), "at least one"), (dict(steps=17), "steps must"), (dict(steps=-1), "steps must"),
     (dict(momentum=-0.1), "momentum"), (dict(momentum=float("nan")), "momentum"), (dict(momentum=0.0), "nesterov"), (dict(eps=-1.0), "eps"),
-    (dict(tile=64), "tile"), (dict(device=-1), "device"), (dict(ld=63), "inside a row"), (dict(matrices=((-1, 8, 8),)), "inside a row"),
+    (dict(tile=64), "tile"), (dict(split=3, tile=128), "split"), (dict(split=2), "split"), (dict(split=2, tile=256), "split"), (dict(device=-1), "device"), (dict(ld=63), "inside a row"), (dict(matrices=((-1, 8, 8),)), "inside a row"),
     (dict(matrices=((0, 0, 8),)), "rows and cols"), (dict(matrices=((0, 8, 1 << 21),)), "rows and cols"), (dict(matrices=((0, 8, 8), (63, 8, 8))), "overlap"),
     (dict(matrices=((0, 8, 8, float("inf")),)), "scale"),
 ])
