@@ -1554,13 +1554,6 @@ void coefficients(const dasgd_ortho_config *c, int &steps, float (*coef)[3]) {
     for (int j = 0; j < 3; ++j) coef[i][j] = c->coefficients ? c->coefficients[3 * i + j] : kDefaultCoef[j];
 }
 
-// CTAs of a tile.  Pairs of CTAs on 256-wide tiles read half as much per operation, single CTAs on 128-wide tiles put four
-// times as many SMs to work.  A tile's loop is bound by what an SM can take in (53 to 60 bytes a cycle), so pairs win as soon as
-// the updates' tiles nearly fill the 74 pairs: one 2048^2 (64 tiles) 402 us against 484 in bfloat16, a block of width 1024
-// (96 tiles) 522 against 630; below that single CTAs: one 1024^2 (16 tiles) 233 us against 258, eight 512^2 (32 tiles) 194
-// against 214.  In float32: 809 / 811, 912 / 1105, 365 / 469, 272 / 336.
-constexpr long long kEnoughTiles = 64;
-
 // All matrices fit SMs (and no tile was asked for).  64 x 96 in float32 takes 30 us instead of 77.
 bool all_small(const dasgd_ortho_config *c) {
   if (c->tile) return false;
@@ -1569,12 +1562,35 @@ bool all_small(const dasgd_ortho_config *c) {
   return true;
 }
 
+// CTAs of a tile.  Pairs of CTAs on 256-wide tiles read half as much per operation; single CTAs on 128-wide tiles put four times
+// as many SMs to work and pad narrow matrices less.  What a step takes is estimated for both, in cycles: a tile's loop by
+// the inner blocks of 64, at least its epilogue, the tiles of a product shared by the SMs (half a round is lost where they take
+// more than one), and the way from product to product.  Measured (us, 128 and 256): bfloat16 1024^2 172, 189; 2048^2 364, 284;
+// six 1024^2 263, 234; 300 of 100 x 300 235, 465; one 4096^2 3300, 1510.  float32 2048^2 604, 586; 2560^2 1234, 989; 64 of 256^2
+// 201, 249; 300 of 100 x 300 293, 721.  Where the estimates are within a tenth of one another, so are the times.
+double step_cycles(const dasgd_ortho_config *c, int cg) {
+  const bool pairs = c->dtype == DASGD_F32;
+  const double slots = 148 / cg, block = cg == 1 ? (pairs ? 1190 : 620) : (pairs ? 1540 : 551), added = pairs && cg == 2 ? 4500 : 0,
+               least = cg == 1 ? (pairs ? 7000 : 5000) : 9500, way = cg == 1 ? 7000 : pairs ? 12000 : 9000;
+  const int64_t tile = 128 * cg;
+  double cycles = 0;
+  for (int phase = 0; phase < 3; ++phase) {
+    double sum = 0, longest = 0, tiles = 0;
+    for (int i = 0; i < c->n_matrices; ++i) {
+      const int64_t n = std::min(c->matrices[i].rows, c->matrices[i].cols), w = std::max(c->matrices[i].rows, c->matrices[i].cols);
+      const double tn = (double)((n + tile - 1) / tile), tw = (double)((w + tile - 1) / tile);
+      const double count = (phase == UPDATE ? tn * tw : tn * (tn + 1) / 2) * c->K;
+      const double one = std::max(least, ((phase == GRAM ? w : n) + kBox - 1) / kBox * block + added);
+      sum += count * one, longest = std::max(longest, one), tiles += count;
+    }
+    cycles += std::max(longest, sum / slots + (tiles > slots ? 0.5 * sum / tiles : 0)) + way;
+  }
+  return cycles;
+}
+
 int choose_tile(const dasgd_ortho_config *c) {
   if (c->tile) return c->tile / 128;
-  long long tiles = 0;
-  for (int i = 0; i < c->n_matrices; ++i)
-    tiles += (long long)((c->matrices[i].rows + 255) / 256) * ((c->matrices[i].cols + 255) / 256);
-  return tiles * c->K >= kEnoughTiles ? 2 : 1;
+  return step_cycles(c, 2) < step_cycles(c, 1) ? 2 : 1;
 }
 
 // CTAs that share a tile's inner dimension, where the tiles of a product leave SMs idle (the caller halves it until all tiles are
