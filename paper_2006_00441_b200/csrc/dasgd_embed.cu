@@ -181,36 +181,47 @@ struct SortArgs {
   uint2 *list[2];             // [K][T] entries (position, key) each; the sorted result is in [passes & 1]
   long long T;
   int V, token_bits, passes, radix_bits, K;
-  int sorted;                 // replicas to sort: K, or 0 without tokens
-  char *grad;                 // the table's gradient, of which grad_bytes of every replica are zeroed
-  long long grad_stride, grad_bytes;
 };
 
-constexpr int kZeroCtas = 148 * 4;    // with the sorting clusters in front they fill the SMs
 constexpr int kMaxCluster = 16;
-constexpr int kZeroPiece = 1 << 16;  // bytes that a CTA zeroes at a time
 
-__device__ __forceinline__ void zero_piece(char *p, int n) {  // n <= kZeroPiece bytes, an even number
+// Shared memory of a sorting CTA, for R values of a digit: counts of the warps' digits, then where their next entry of a digit
+// goes [kSortWarps][R]; totals of every CTA of the cluster, which writes them here [kMaxCluster][R]; a scan's [kSortWarps].
+constexpr int sort_shared_bytes(int radix_bits) { return (((kSortWarps + kMaxCluster) << radix_bits) + kSortWarps) * 4; }
+
+// Zeroes the table's gradient in every replica.  It runs beside the sort, which keeps a few SMs busy with latencies (rows that
+// tokens select are written once more by the sums: cheaper than waiting to know which).  Many short CTAs: 262 MB take 36 us;
+// four CTAs to an SM that go through it in pieces take 49.
+constexpr int kZeroThreads = 256, kZeroPiece = kZeroThreads * 16 * 4;  // bytes of a CTA
+
+struct ZeroArgs {
+  char *grad;
+  long long stride, bytes;  // from replica to replica, of a replica
+  long long per;            // pieces of a replica
+};
+
+__global__ void __launch_bounds__(kZeroThreads) k_embed_zero(const ZeroArgs a) {
+  asm volatile("griddepcontrol.launch_dependents;");
+  const long long k = blockIdx.x / a.per, at = (blockIdx.x - k * a.per) * kZeroPiece;
+  char *p = a.grad + k * a.stride + at;
+  const int n = (int)min((long long)kZeroPiece, a.bytes - at);  // an even number, as the address is
   const int head = min(n, (int)(-reinterpret_cast<uintptr_t>(p) & 15)), body = (n - head) / 16, tail = n - head - body * 16;
   if (threadIdx.x < head / 2) reinterpret_cast<uint16_t *>(p)[threadIdx.x] = 0;
   uint4 *q = reinterpret_cast<uint4 *>(p + head);
-#pragma unroll 8
-  for (int i = threadIdx.x; i < body; i += kSortThreads) __stcs(q + i, make_uint4(0, 0, 0, 0));
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    if (threadIdx.x + j * kZeroThreads < body) __stcs(q + threadIdx.x + j * kZeroThreads, make_uint4(0, 0, 0, 0));
   if (threadIdx.x < tail / 2) reinterpret_cast<uint16_t *>(q + body)[threadIdx.x] = 0;
+  // The kernel after this one waits for this one alone: it ends no sooner than the sort before it.
+  if (blockIdx.x == 0) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
-// The first K clusters each sort one replica's tokens: a stable radix sort from the lowest digit up, `passes` digits of
+// A cluster sorts one replica's tokens: a stable radix sort from the lowest digit up, `passes` digits of
 // `radix_bits` bits.  Every CTA owns a contiguous part of the sequence and every warp a contiguous part of that, so the order
 // within a digit is (CTA, warp, round, lane) = the order of the sequence.  Tokens outside the table get the key V and sort to
 // the end.  All passes run in one launch: the digit counts cross CTAs through distributed shared memory, the keys
 // through L2, and a cluster barrier (about a microsecond) stands where a launch boundary would.
 //
-// Sorting keeps a few SMs busy with latencies.  The clusters after the first K meanwhile zero the whole table of every replica
-// (rows that tokens select are written once more by the sums: cheaper than waiting to know which).
-// Shared memory of a sorting CTA, for R values of a digit: counts of the warps' digits, then where their next entry of a digit
-// goes [kSortWarps][R]; totals of every CTA of the cluster, which writes them here [kMaxCluster][R]; a scan's [kSortWarps].
-constexpr int sort_shared_bytes(int radix_bits) { return (((kSortWarps + kMaxCluster) << radix_bits) + kSortWarps) * 4; }
-
 // kBatch: entries of a lane that are loaded and voted on together; a warp whose part is no longer than that holds it in
 // registers from the counting to the placing.
 template <int kBatch>
@@ -221,14 +232,6 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_tokens(const SortArgs a) 
   const int nC = cluster.num_blocks(), rank = cluster.block_rank();
   const long long k = blockIdx.x / nC;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  if (k >= a.sorted) {
-    const long long per = (a.grad_bytes + kZeroPiece - 1) / kZeroPiece, all = per * a.K;
-    for (long long i = blockIdx.x - (long long)a.sorted * nC; i < all; i += gridDim.x - (long long)a.sorted * nC) {
-      const long long at = i % per * kZeroPiece;
-      zero_piece(a.grad + i / per * a.grad_stride + at, (int)min((long long)kZeroPiece, a.grad_bytes - at));
-    }
-    return;
-  }
   const int R = 1 << a.radix_bits;
   uint32_t *hist = sort_shared + warp * R, *hists = sort_shared, *totals = hists + kSortWarps * R, *scan = totals + kMaxCluster * R;
   const uint32_t none = (uint32_t)a.V;
@@ -999,15 +1002,19 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   so.tokens = tokens;
   for (int i = 0; i < 2; ++i) so.list[i] = reinterpret_cast<uint2 *>(ws + p.list[i]);
   so.T = c.T, so.V = c.V, so.token_bits = c.token_bits, so.passes = p.passes, so.radix_bits = p.radix_bits;
-  so.K = c.K, so.sorted = c.T ? c.K : 0;
+  so.K = c.K;
   char *grad = static_cast<char *>(grad_array) + c.offset * size_of(c.table_elem);
-  long long zero_ctas = 0;
-  if (!c.accumulate) {
-    so.grad = grad, so.grad_stride = c.ld * size_of(c.table_elem), so.grad_bytes = (long long)c.V * c.D * size_of(c.table_elem);
-    zero_ctas = std::min<long long>(kZeroCtas, c.K * ((so.grad_bytes + kZeroPiece - 1) / kZeroPiece));
+  cudaError_t e = cudaSuccess;
+  ZeroArgs zero{grad, c.ld * (long long)size_of(c.table_elem), (long long)c.V * c.D * (long long)size_of(c.table_elem), 0};
+  zero.per = (zero.bytes + kZeroPiece - 1) / kZeroPiece;
+  if (zero.per * c.K > INT32_MAX) return dasgd_internal_fail(nullptr, DASGD_ERR_UNSUPPORTED, "embed_gradient: K*V*D too large for one launch");
+  if (!c.T) {
+    k_embed_zero<<<(unsigned)(zero.per * c.K), kZeroThreads, 0, s>>>(zero);
+    e = cudaGetLastError();
+    return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "embed_gradient: zeroing");
   }
   cudaLaunchConfig_t lc{};
-  lc.gridDim = dim3((unsigned)(so.sorted * p.cluster + (zero_ctas + p.cluster - 1) / p.cluster * p.cluster));
+  lc.gridDim = dim3((unsigned)(c.K * p.cluster));
   lc.blockDim = dim3(kSortThreads);
   lc.stream = s;
   cudaLaunchAttribute attr[1];
@@ -1017,11 +1024,12 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   lc.dynamicSmemBytes = sort_shared_bytes(p.radix_bits);
   const long long rounds = (c.T + (long long)p.cluster * kSortThreads - 1) / ((long long)p.cluster * kSortThreads);
   auto kernel = rounds <= 1 ? k_sort_tokens<1> : rounds <= 2 ? k_sort_tokens<2> : rounds <= 4 ? k_sort_tokens<4> : k_sort_tokens<8>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sort_shared_bytes(p.radix_bits));
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sort_shared_bytes(p.radix_bits));
   if (e == cudaSuccess && p.cluster > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   if (e == cudaSuccess) e = cudaLaunchKernelEx(&lc, kernel, so);
   if (e != cudaSuccess) return cuda_fail(e, "embed_gradient: sort");
-  if (!c.T) return DASGD_OK;
+  if (!c.accumulate && (e = launch_after(k_embed_zero, dim3((unsigned)(zero.per * c.K)), kZeroThreads, 0, s, zero)) != cudaSuccess)
+    return cuda_fail(e, "embed_gradient: zeroing");
 
   GradArgs a{};
   a.dy = dy;
