@@ -443,7 +443,7 @@ class Embedding:
             elem = _ELEM.get(out_dtype or w.dtype)
             if elem is None:
                 raise ValueError("out_dtype must be float32 or bfloat16")
-            out = torch.empty((self.K, T, self.D), dtype=out_dtype or w.dtype, device=self.device)
+            out = w.new_empty((self.K, T, self.D), dtype=out_dtype or w.dtype)
             self.cfg.rows_elem = elem
         else:
             self._rows(out, T)

@@ -382,6 +382,7 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   const uint2 *list = a.list + k * a.T;
   const long long e0 = (long long)b * a.blk, e1 = min(a.T, e0 + a.blk);
   const uint32_t first = list[e0].y, prev = e0 ? list[e0 - 1].y : none, next = e1 < a.T ? list[e1].y : none;
+  uint2 ahead = e0 + lane < e1 ? list[e0 + lane] : make_uint2(0, none);
   if (first == none) return;
   const int c0 = s * kSliceCols + lane * VEC;
   int col[NV];  // this lane's columns; the ones beyond D are read at column 0 and not written
@@ -395,10 +396,11 @@ __device__ __forceinline__ void sum_block(const GradArgs &a, long long task) {
   bool head = prev == first;  // the first run of the block began earlier
   for (long long e = e0; e < e1; e += 32) {
     const int n = (int)min(32LL, e1 - e);
-    const uint2 entry = lane < n ? list[e + lane] : make_uint2(0, none);
-    const uint32_t kl = entry.y, pl = entry.x;
+    const uint32_t kl = ahead.y, pl = ahead.x;
+    ahead = e + 32 + lane < e1 ? list[e + 32 + lane] : make_uint2(0, none);
     uint32_t follow = __shfl_down_sync(0xffffffffu, kl, 1);
-    if (lane == 31) follow = e + 32 < e1 ? list[e + 32].y : none;
+    const uint32_t beyond = __shfl_sync(0xffffffffu, ahead.y, 0);
+    if (lane == 31) follow = beyond;
     const bool last = e + lane == e1 - 1;
     // what an entry does when it has been added: 0 nothing, 1 its run ends in the block, 2 its run goes on in the next one
     const int what = kl == none || (!last && follow == kl) ? 0 : last && next == kl ? 2 : 1;
@@ -734,13 +736,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
       if ((number + f) % kShare != unit % kShare) continue;
       const int b = found[f];
       const uint32_t v = list[(long long)b * a.blk + a.blk - 1].y;
-      int lo = b + kLong + 1, hi = a.blocks;  // the last block whose first token is v: binary search, the tokens are sorted
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (list[(long long)mid * a.blk].y == v) lo = mid;
-        else hi = mid;
-      }
-      const int n = lo - b + 1;
+      int n = kLong + 1;  // parts: the blocks whose first token is v follow one another
+      for (int at = b + kLong + 1, more = kJoinThreads; more == kJoinThreads; at += kJoinThreads, n += more)
+        more = __syncthreads_count(at + tid < a.blocks && list[(long long)min(at + tid, a.blocks - 1) * a.blk].y == v);
       const float *part = parts(b) + (c < a.D ? c : 0);
       float acc[VEC] = {};
       for (int i0 = warp; i0 < n; i0 += 8 * kJoinWarps) {
@@ -777,18 +775,18 @@ __global__ void __launch_bounds__(kJoinThreads) k_embed_join(const GradArgs a) {
 dasgd_status bad(const std::string &m) { return dasgd_internal_fail(nullptr, DASGD_ERR_INVALID_ARG, m.c_str()); }
 
 dasgd_status check(const dasgd_embed_config *c, const char *who) {
-  const std::string at = std::string(who) + ": ";
-  if (!c) return bad(at + "cfg is NULL");
-  if (c->K < 1 || c->K > 65535) return bad(at + "K must be in [1, 65535]");
-  if (c->V < 1 || c->V == INT32_MAX) return bad(at + "V must be in [1, 2^31 - 2]");
-  if (c->D < 1 || c->D > (1 << 22)) return bad(at + "D must be in [1, 2^22]");
-  if (c->T < 0 || c->T >= (1LL << 31)) return bad(at + "T must be in [0, 2^31)");
+  const auto refuse = [who](const char *why) { return bad(std::string(who) + ": " + why); };
+  if (!c) return refuse("cfg is NULL");
+  if (c->K < 1 || c->K > 65535) return refuse("K must be in [1, 65535]");
+  if (c->V < 1 || c->V == INT32_MAX) return refuse("V must be in [1, 2^31 - 2]");
+  if (c->D < 1 || c->D > (1 << 22)) return refuse("D must be in [1, 2^22]");
+  if (c->T < 0 || c->T >= (1LL << 31)) return refuse("T must be in [0, 2^31)");
   if (c->offset < 0 || c->ld < 1 || c->offset > c->ld || (int64_t)c->V * c->D > c->ld - c->offset)
-    return bad(at + "the table must lie inside a row: offset >= 0, offset + V*D <= ld");
-  if (c->token_bits != 32 && c->token_bits != 64) return bad(at + "token_bits must be 32 or 64");
-  if ((c->table_elem | 1) != 1 || (c->rows_elem | 1) != 1) return bad(at + "unknown element type");
-  if (!isfinite(c->scale)) return bad(at + "scale must be finite");
-  if (c->device < 0) return bad(at + "device must be >= 0");
+    return refuse("the table must lie inside a row: offset >= 0, offset + V*D <= ld");
+  if (c->token_bits != 32 && c->token_bits != 64) return refuse("token_bits must be 32 or 64");
+  if ((c->table_elem | 1) != 1 || (c->rows_elem | 1) != 1) return refuse("unknown element type");
+  if (!isfinite(c->scale)) return refuse("scale must be finite");
+  if (c->device < 0) return refuse("device must be >= 0");
   return DASGD_OK;
 }
 
