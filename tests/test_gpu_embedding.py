@@ -183,6 +183,28 @@ def test_calls_on_different_streams_share_the_workspace_safely():
         assert bool(((g.view(K, V, D).double() - want).abs() <= bound).all())
 
 
+@pytest.mark.parametrize("acc", [False, True])
+def test_replays_of_a_captured_call(acc):
+    from paper_2006_00441_b200 import binding as B
+    K, T, V, D = 2, 3000, 700, 136
+    gen, tok, ld = make(K, T, V, D, 8)
+    dy = torch.randn(K, T, D, generator=gen, device="cuda")
+    emb = B.Embedding(K, ld, 8, V, D, max_tokens=T)
+    start = torch.randn(K, ld, generator=gen, device="cuda")
+    want, g = start.clone(), start.clone()
+    emb.gradient(dy, tok, want, accumulate=acc)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        emb.gradient(dy, tok, g, accumulate=acc)
+        y = emb.lookup(g, tok)
+    for _ in range(3):
+        g.copy_(start)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(g, want) and torch.equal(y, emb.lookup(want, tok))
+
+
 def test_a_gradient_array_beyond_two_to_the_31_elements():
     """Offsets past 32 bits: the second replica's table lies beyond element 2^31 of the array."""
     from paper_2006_00441_b200 import binding as B

@@ -164,6 +164,41 @@ def test_other_polynomials(coef, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tile", [0, 128, 256])
+def test_more_shapes_than_shared_memory_holds(tile, dtype):
+    check([(40 + 13 * i, 300 - 17 * i) for i in range(12)] + [(131, 40), (131, 40)], K=2, dtype=dtype, tile=tile, gap=1)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("steps", [1, 2, 16])
+@pytest.mark.parametrize("r,c", [(60, 100), (260, 180)])
+def test_numbers_of_steps(steps, r, c, dtype):
+    check([(r, c)], dtype=dtype, steps=steps, coef=(1.5, -0.5, 0.0), kind="flat")
+
+
+@pytest.mark.parametrize("r,c", [(64, 96), (300, 200), (1024, 1024), (2048, 2304)])
+def test_replays_of_a_captured_call(r, c):
+    from paper_2006_00441_b200 import binding as B
+    g = torch.randn(2, r * c, device="cuda")
+    op = B.Ortho(2, r * c, [(0, r, c)], momentum=0.0)
+    want = op.step(g, out=torch.empty_like(g)).clone()
+    op.sync()
+    out = torch.zeros_like(g)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        op.step(g, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    g.mul_(-2.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, -want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_zero_matrix_gives_zero_and_nan_stays_in_its_matrix(dtype):
     from paper_2006_00441_b200 import binding as B
     K, n = 3, 130
