@@ -1562,16 +1562,16 @@ bool all_small(const dasgd_ortho_config *c) {
   return true;
 }
 
-// CTAs of a tile.  Pairs of CTAs on 256-wide tiles read half as much per operation; single CTAs on 128-wide tiles put four times
-// as many SMs to work and pad narrow matrices less.  What a step takes is estimated for both, in cycles: a tile's loop by
-// the inner blocks of 64, at least its epilogue, the tiles of a product shared by the SMs (half a round is lost where they take
-// more than one), and the way from product to product.  Measured (us, 128 and 256): bfloat16 1024^2 172, 189; 2048^2 364, 284;
-// six 1024^2 263, 234; 300 of 100 x 300 235, 465; one 4096^2 3300, 1510.  float32 2048^2 604, 586; 2560^2 1234, 989; 64 of 256^2
-// 201, 249; 300 of 100 x 300 293, 721.  Where the estimates are within a tenth of one another, so are the times.
-double step_cycles(const dasgd_ortho_config *c, int cg) {
+// What a step takes with tiles of cg CTAs side by side, or of sk CTAs that share the inner dimension, estimated in cycles: a tile's
+// loop by its inner blocks of 64, at least its epilogue; the tiles of a product divided among the clusters (half a round is lost
+// where they take more than one); the way from product to product.  Measured: a block takes a CTA 620 cycles, what an SM can
+// take in, or 1190 where operands are pairs, and 551 or 1540 on 256-wide tiles; handing partial sums over costs 2500 cycles between
+// two CTAs, 6400 between four.  Clusters of four leave some SMs of a GPC idle.
+double step_cycles(const dasgd_ortho_config *c, int cg, int sk) {
   const bool pairs = c->dtype == DASGD_F32;
-  const double slots = 148 / cg, block = cg == 1 ? (pairs ? 1190 : 620) : (pairs ? 1540 : 551), added = pairs && cg == 2 ? 4500 : 0,
-               least = cg == 1 ? (pairs ? 7000 : 5000) : 9500, way = cg == 1 ? 7000 : pairs ? 12000 : 9000;
+  const double slots = sk == 4 ? 33 : 148 / (cg * sk), block = (cg == 1 ? (pairs ? 1190 : 620) : (pairs ? 1540 : 551)) / (double)sk,
+               added = (pairs && cg == 2 ? 4500 : 0) + (sk == 4 ? 6400 : sk == 2 ? 2500 : 0), least = cg == 1 ? (pairs ? 7000 : 5000) : 9500,
+               way = cg == 1 ? 7000 : pairs ? 12000 : 9000;
   const int64_t tile = 128 * cg;
   double cycles = 0;
   for (int phase = 0; phase < 3; ++phase) {
@@ -1580,7 +1580,7 @@ double step_cycles(const dasgd_ortho_config *c, int cg) {
       const int64_t n = std::min(c->matrices[i].rows, c->matrices[i].cols), w = std::max(c->matrices[i].rows, c->matrices[i].cols);
       const double tn = (double)((n + tile - 1) / tile), tw = (double)((w + tile - 1) / tile);
       const double count = (phase == UPDATE ? tn * tw : tn * (tn + 1) / 2) * c->K;
-      const double one = std::max(least, ((phase == GRAM ? w : n) + kBox - 1) / kBox * block + added);
+      const double one = std::max(least, ((phase == GRAM ? w : n) + kBox - 1) / kBox * block) + added;
       sum += count * one, longest = std::max(longest, one), tiles += count;
     }
     cycles += std::max(longest, sum / slots + (tiles > slots ? 0.5 * sum / tiles : 0)) + way;
@@ -1588,24 +1588,27 @@ double step_cycles(const dasgd_ortho_config *c, int cg) {
   return cycles;
 }
 
-int choose_tile(const dasgd_ortho_config *c) {
-  if (c->tile) return c->tile / 128;
-  return step_cycles(c, 2) < step_cycles(c, 1) ? 2 : 1;
-}
+struct Division {
+  int cg, sk;
+};
 
-// CTAs that share a tile's inner dimension, where the tiles of a product leave SMs idle (the caller halves it until all tiles are
-// resident at once).  A 64-wide block of the inner dimension takes a CTA 620 cycles, or 1190 where operands are pairs; handing
-// partial sums over costs a product 2500 cycles between two CTAs and 6400 between four.  The longest of the matrices has
-// (w + 2 n) / 64 blocks in a step's three products.  One CTA, two, four (us): float32 256^2 124, 131, 152; 300 x 600 157, 154, 166;
-// 768^2 217, 187; 1024^2 269, 220; 100 x 4000 328, 239, 206.  bfloat16 768^2 142, 148; 1024^2 172, 167; 100 x 4000 199, 174, 169.
-int choose_split(const dasgd_ortho_config *c) {
-  int blocks = 0;
-  for (int i = 0; i < c->n_matrices; ++i) {
-    const dasgd_matrix &m = c->matrices[i];
-    blocks = std::max(blocks, (std::max(m.rows, m.cols) + 2 * std::min(m.rows, m.cols)) / kBox);
+// Pairs of CTAs on 256-wide tiles read half as much per operation; single CTAs on 128-wide tiles put four times as many SMs to work and
+// pad narrow matrices less; CTAs that share a tile's inner dimension shorten the products of few tiles and long sums.  The least
+// estimate is taken.  Measured (us, 128 and 256): bfloat16 1024^2 172, 189; 2048^2 364, 284; six 1024^2 263, 234; 300 of 100 x 300
+// 235, 465; one 4096^2 3300, 1510.  float32 2048^2 604, 586; 2560^2 1234, 989; 64 of 256^2 201, 249; 300 of 100 x 300 293, 721.
+// One CTA, two, four: float32 256^2 124, 131, 152; 300 x 600 157, 154, 166; 768^2 217, 187; 1500^2 381, 430, 526; 100 x 4000 328, 239,
+// 206; five 64 x 8000 568, 415, 464; bfloat16 768^2 142, 148; 1024^2 172, 167; 100 x 4000 199, 174, 169; 64 of 200 x 300 141, 262.  Where
+// estimates are within a tenth of one another, so are the times.
+Division divide(const dasgd_ortho_config *c) {
+  if (c->split) return {1, c->split};
+  Division best{1, 1};
+  double least = INFINITY;
+  for (const Division &d : {Division{1, 1}, {1, 2}, {1, 4}, {2, 1}}) {
+    if (c->tile && c->tile != 128 * d.cg) continue;
+    const double cycles = step_cycles(c, d.cg, d.sk);
+    if (cycles < least) best = d, least = cycles;
   }
-  if (c->dtype == DASGD_F32) return blocks >= 40 ? 4 : blocks >= 18 ? 2 : 1;
-  return blocks >= 60 ? 4 : blocks >= 48 ? 2 : 1;
+  return best;
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -1696,7 +1699,7 @@ dasgd_status dasgd_ortho_workspace(const dasgd_ortho_config *cfg, int64_t *bytes
   if (!bytes) return bad("ortho_workspace: bytes is NULL");
   try {
     Layout l;
-    st = layout(cfg, "ortho_workspace", choose_tile(cfg), l);
+    st = layout(cfg, "ortho_workspace", divide(cfg).cg, l);
     if (st == DASGD_OK) *bytes = (int64_t)l.bytes;
     return st;
   } catch (const std::bad_alloc &) {
@@ -1714,7 +1717,7 @@ dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, 
   coefficients(cfg, p.steps, p.coef);
   if (!bounded(p.coef, p.steps))
     return unsupported("ortho_init: these coefficients let the iterates grow past the range of the fp16 operands");
-  const int cg = choose_tile(cfg);
+  const auto [cg, sk] = divide(cfg);
   Layout l;
   st = layout(cfg, "ortho_init", cg, l);
   if (st != DASGD_OK) return st;
@@ -1768,31 +1771,26 @@ dasgd_status dasgd_ortho_init(dasgd_ortho **out, const dasgd_ortho_config *cfg, 
   p.mu = c.momentum, p.eps = c.eps, p.nesterov = c.nesterov != 0;
   p.timeout_ns = (c.timeout_ms ? c.timeout_ms : 10000u) * 1000000ull;
 
-  // CTAs that may share a tile: as many as leave all tiles of a product resident at once
-  int sms = 0, sk = c.split ? c.split : cg == 1 ? choose_split(cfg) : 1;
+  int sms = 0, clusters = 0;
   if ((e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, c.device)) != cudaSuccess) return cuda_fail(e, "ortho_init");
-  long long room = 0;
-  for (;; sk /= 2) {
-    int clusters = 0;
-    st = with_kernel(cg, sk, c.dtype, [&](auto kernel, auto *) -> dasgd_status {
-      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
-      if (e == cudaSuccess && cg * sk > 1) {
-        cudaLaunchConfig_t lc;
-        cudaLaunchAttribute attr[2];
-        launch_config(lc, attr, cg * sk, sms / (cg * sk) * (cg * sk), s);
-        e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
-      }
-      return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "ortho_init");
-    });
-    if (st != DASGD_OK) return st;
-    room = cg * sk > 1 ? std::min(clusters, sms / (cg * sk)) : sms;
-    if (c.split || sk == 1 || room >= l.most_tiles) break;
-  }
+  const int ctas = cg * sk;
+  st = with_kernel(cg, sk, c.dtype, [&](auto kernel, auto *) -> dasgd_status {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+    if (e == cudaSuccess && ctas > 1) {
+      cudaLaunchConfig_t lc;
+      cudaLaunchAttribute attr[2];
+      launch_config(lc, attr, ctas, sms / ctas * ctas, s);
+      e = cudaOccupancyMaxActiveClusters(&clusters, kernel, &lc);
+    }
+    return e == cudaSuccess ? DASGD_OK : cuda_fail(e, "ortho_init");
+  });
+  if (st != DASGD_OK) return st;
+  const long long room = ctas > 1 ? std::min(clusters, sms / ctas) : sms;
   if (room < 1) return unsupported("ortho_init: the kernel does not fit this GPU");
   dasgd_ortho *op = new dasgd_ortho;
   op->plan = p, op->device = c.device, op->dtype = c.dtype, op->cg = cg, op->sk = sk, op->chunks = l.chunks, op->rblks = l.rblks;
   op->has_momentum = c.momentum != 0.0f;
-  op->grid = (int)std::min(l.most_tiles, room) * cg * sk;
+  op->grid = (int)std::min(l.most_tiles, room) * ctas;
   if (all_small(cfg)) {
     e = c.dtype == DASGD_F32 ? cudaFuncSetAttribute(k_ortho_small<true, float>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallShared))
                              : cudaFuncSetAttribute(k_ortho_small<false, __nv_bfloat16>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(SmallShared));
