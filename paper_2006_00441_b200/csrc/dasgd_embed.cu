@@ -135,7 +135,8 @@ __device__ __forceinline__ long long token_at(const void *tokens, int bits, long
 
 // A CTA is 2^xs threads across a row (units of VEC elements) by 256 >> xs rows, and takes kRows such sets of rows, 64 bytes of
 // the table in flight for each thread.  Six CTAs to an SM (42 registers) matter more than rows in flight: 4 x 32768 rows of
-// 1024 bfloat16 took 74 us with four CTAs, 98 us with two and twice the rows, 85 us as a pipeline of persistent CTAs.
+// 1024 bfloat16 take 64 us (4.2 TB/s of stores, which bound it); 74 with four CTAs, 98 with two and twice the rows, 85 as a pipeline of
+// persistent CTAs.
 template <typename W, typename O, int VEC>
 __global__ void __launch_bounds__(kThreads, VEC == 8 ? 6 : 4) k_embed_lookup(const LookupArgs a) {
   constexpr int kRows = lookup_rows<W, VEC>();
