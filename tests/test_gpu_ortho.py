@@ -111,6 +111,13 @@ def test_tiles_whose_inner_dimension_is_shared(shapes, K, split, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("shapes,K", [([(64, 8000)], 5), ([(3411, 59), (978, 48), (106, 4079)], 2), ([(2050, 130), (70, 66)], 1), ([(160, 1500), (1100, 1100)], 2)])
+def test_long_matrices_beside_short_ones(shapes, K, dtype):
+    """Products of few tiles and long sums, and products of more tiles than the GPU holds, in one call."""
+    check(shapes, K=K, dtype=dtype, gap=5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("kind", ["flat", "noisy", "decaying"])
 @pytest.mark.parametrize("r,c", [(1, 1), (1, 256), (256, 1), (2, 3), (8, 8), (15, 17), (63, 65), (64, 64), (65, 64), (64, 96), (100, 200), (200, 100), (127, 129), (128, 128),
                                  (128, 256), (256, 128), (129, 127), (33, 255)])
