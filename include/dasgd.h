@@ -366,10 +366,10 @@ dasgd_status dasgd_embed_lookup(const dasgd_embed_config *cfg, const void *table
                                 void *out_device, void *stream);
 
 /* dtable_k[v][:] (+)= scale * sum over t with tokens[k][t] = v of dy[k][t][:].  Tokens are sorted on the device,
- * sums are held in float32 and added in an order that the tokens alone decide (no floating-point atomics: equal
- * inputs give equal bits), and rounded once.  Tokens outside [0, V) contribute nothing.  workspace: device, 256-byte
- * aligned, of at least the bytes that dasgd_embed_workspace names (they serve any T up to cfg->T); its contents need not be kept between calls, and calls
- * that can overlap on the GPU need one each. */
+ * sums are held in float32 and added in an order that the tokens alone decide (no atomics whose order could matter:
+ * equal inputs give equal bits), and rounded once.  Tokens outside [0, V) contribute nothing.  workspace: device,
+ * 256-byte aligned, of at least the bytes that dasgd_embed_workspace names (they serve any T up to cfg->T; T = 0 needs
+ * none); its contents need not be kept between calls, and calls that can overlap on the GPU need one each. */
 dasgd_status dasgd_embed_workspace(const dasgd_embed_config *cfg, int64_t *bytes);
 dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy_device, const void *tokens_device,
                                   void *grad_array_device, void *workspace_device, int64_t workspace_bytes, void *stream);

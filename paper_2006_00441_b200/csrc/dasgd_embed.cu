@@ -985,7 +985,7 @@ dasgd_status dasgd_embed_gradient(const dasgd_embed_config *cfg, const void *dy,
   const Plan p = plan(c, vec == 8);
   if (c.T == 0 && c.accumulate) return DASGD_OK;
   if (!grad_array || (c.T && (!dy || !tokens))) return bad("embed_gradient: dy, tokens and grad_array must not be NULL");
-  if (!workspace || !aligned(workspace, 256) || workspace_bytes < (int64_t)p.bytes)
+  if (c.T && (!workspace || !aligned(workspace, 256) || workspace_bytes < (int64_t)p.bytes))
     return bad("embed_gradient: needs a 256-byte aligned workspace of " + std::to_string(p.bytes) + " bytes");
   if (!aligned(grad_array, size_of(c.table_elem)) || !aligned(dy, size_of(c.rows_elem)) || !aligned(tokens, c.token_bits / 8))
     return bad("embed_gradient: buffers must be aligned to their elements");

@@ -235,3 +235,19 @@ def test_wrapper_refuses_what_it_cannot_take():
             bad()
     with pytest.raises(B.DasgdError):
         B.Embedding(2, 63, 0, 8, 8)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("max_tokens", [0, 7])
+def test_no_tokens_with_and_without_a_workspace(max_tokens, accumulate):
+    from paper_2006_00441_b200 import binding as B
+    K, V, D, ld = 2, 5, 3, 21
+    emb = B.Embedding(K, ld, 4, V, D, max_tokens=max_tokens)
+    g = torch.full((K, ld), 3.0, device="cuda")
+    tokens = torch.empty(K, 0, dtype=torch.int64, device="cuda")
+    emb.gradient(torch.empty(K, 0, D, device="cuda"), tokens, g, accumulate=accumulate)
+    want = torch.full((K, ld), 3.0, device="cuda")
+    if not accumulate:
+        want[:, 4:4 + V * D] = 0.0
+    assert torch.equal(g, want)
+    assert emb.lookup(g, tokens).shape == (K, 0, D)
