@@ -251,3 +251,35 @@ def test_no_tokens_with_and_without_a_workspace(max_tokens, accumulate):
         want[:, 4:4 + V * D] = 0.0
     assert torch.equal(g, want)
     assert emb.lookup(g, tokens).shape == (K, 0, D)
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 66, 33])
+@pytest.mark.parametrize("T", [5, 700, 9000])
+def test_nan_in_rows_that_count_for_nothing(T, D, dt, accumulate):
+    """NaN in rows of dy without a token of the table, in rows of the gradient that are not added to, and in a workspace never
+    written before leaves the sums as they are (whole numbers below 2^8: exact in every type and order)."""
+    from paper_2006_00441_b200 import binding as B
+    K, V = 2, 97
+    gen = torch.Generator("cuda").manual_seed(T + D)
+    tokens = torch.randint(0, V // 2, (K, T), generator=gen, device="cuda")
+    dy = torch.zeros(K, T, D, device="cuda")
+    one = torch.arange(0, T, max(1, T // 40), device="cuda")     # few rows that are not zero
+    dy[:, one] = 1.0
+    none = torch.rand(K, T, generator=gen, device="cuda") < 0.2
+    tokens[none] = torch.where(torch.rand(K, T, generator=gen, device="cuda") < 0.5, -1, V)[none]
+    want = torch.zeros(K, V, D, device="cuda")
+    for k in range(K):
+        want[k].index_add_(0, tokens[k][~none[k]], dy[k][~none[k]])
+    dy[none] = float("nan")
+    g = torch.full((K, V, D), float("nan"), device="cuda")
+    if accumulate:
+        g[:, :V // 2] = 2.0
+        want += 2.0
+        want[:, V // 2:] = float("nan")
+    g = g.to(dt)
+    emb = B.Embedding(K, V * D, 0, V, D, max_tokens=T)
+    emb._ws.fill_(255)
+    emb.gradient(dy.to(dt), tokens, g.view(K, V * D), accumulate=accumulate)
+    assert torch.equal(g.float().nan_to_num(-7.0), want.nan_to_num(-7.0))
