@@ -126,30 +126,34 @@ struct LookupArgs {
   long long ld, T;
   int V, D, token_bits;
   float scale;
-  int xs;              // log2 of the threads of a CTA that share a row
+  int xs, X, Y;        // threads of a CTA across a row (2^xs or X), rows that they cover at a time
 };
 
 __device__ __forceinline__ long long token_at(const void *tokens, int bits, long long i) {
   return bits == 64 ? __ldg(static_cast<const long long *>(tokens) + i) : (long long)__ldg(static_cast<const int *>(tokens) + i);
 }
 
-// A CTA is 2^xs threads across a row (units of VEC elements) by 256 >> xs rows, and takes kRows such sets of rows, 64 bytes of
-// the table in flight for each thread.  Six CTAs to an SM (42 registers) matter more than rows in flight: 4 x 32768 rows of
-// 1024 bfloat16 take 64 us (4.2 TB/s of stores, which bound it); 74 with four CTAs, 98 with two and twice the rows, 85 as a pipeline of
-// persistent CTAs.
-template <typename W, typename O, int VEC>
+// A CTA is X threads across a row (units of VEC elements) by Y rows, and takes kRows such sets of rows, 64 bytes of the table in
+// flight for each thread.  Six CTAs to an SM (42 registers) matter more than rows in flight: 4 x 32768 rows of 1024 bfloat16 take
+// 64 us (4.2 TB/s of stores, which bound it); 74 with four CTAs, 98 with two and twice the rows, 85 as a pipeline of persistent CTAs.
+// X is what a row needs: with powers of two, 32 at least, idle threads took 4 x 50000 rows of 7 float32 29 us instead of 9, of 75
+// 33 instead of 25, of 136 bfloat16 25 instead of 19.  Where rows are aligned and a power of two leaves no less rows at a time, it
+// is taken: its shifts save the registers that spill otherwise (the 64 us were 72).
+template <typename W, typename O, int VEC, bool SHIFT>
 __global__ void __launch_bounds__(kThreads, VEC == 8 ? 6 : 4) k_embed_lookup(const LookupArgs a) {
   constexpr int kRows = lookup_rows<W, VEC>();
-  const int X = 1 << a.xs, Y = kThreads >> a.xs;
-  const int tx = threadIdx.x & (X - 1), ty = threadIdx.x >> a.xs;
+  const int X = SHIFT ? 1 << a.xs : a.X, Y = SHIFT ? kThreads >> a.xs : a.Y;
+  const int ty = SHIFT ? threadIdx.x >> a.xs : threadIdx.x / (unsigned)X, tx = (int)threadIdx.x - ty * X;
+  if (!SHIFT && ty >= Y) return;
   const long long k = blockIdx.y, t0 = (long long)blockIdx.x * (Y * kRows) + ty;
   const W *table = static_cast<const W *>(a.table) + k * a.ld;
   O *out = static_cast<O *>(a.out) + (k * a.T + t0) * a.D;
-  const int live = (int)min((long long)kRows, (a.T - t0 + Y - 1) / Y);  // rows of this thread; may be <= 0
+  const int left = (int)(a.T - t0), live = SHIFT ? (left + Y - 1) >> (31 - __clz(kThreads) - a.xs) : 0;  // may be <= 0
+  const auto exists = [=](int j) { return SHIFT ? j < live : j * Y < left; };
   int tok[kRows];  // -1: none of the table's rows
 #pragma unroll
   for (int j = 0; j < kRows; ++j) {
-    const long long t = j < live ? token_at(a.tokens, a.token_bits, k * a.T + t0 + (long long)j * Y) : -1;
+    const long long t = exists(j) ? token_at(a.tokens, a.token_bits, k * a.T + t0 + (long long)j * Y) : -1;
     tok[j] = t >= 0 && t < a.V ? (int)t : -1;
   }
   constexpr int kAcross = VEC == 8 ? 1 : 4;  // units of a row that a thread has in flight
@@ -164,7 +168,7 @@ __global__ void __launch_bounds__(kThreads, VEC == 8 ? 6 : 4) k_embed_lookup(con
     for (int u = 0; u < kAcross; ++u)
 #pragma unroll
       for (int j = 0; j < kRows; ++j) {
-        if (j >= live || c + u * X * VEC >= a.D) continue;
+        if (!exists(j) || c + u * X * VEC >= a.D) continue;
         if (tok[j] < 0) raw[u][j].clear();
         float x[VEC];
         raw[u][j].widen(x);
@@ -889,15 +893,16 @@ Plan plan(const dasgd_embed_config &c, bool vec) {
 
 template <typename W, typename O>
 void launch_lookup(const dasgd_embed_config &c, LookupArgs a, int vec, cudaStream_t s) {
-  // threads of a row: a power of two, as many as it has units, or a quarter where a thread takes four of them
-  const int units = c.D / vec, want = vec == 8 ? units : (units + 3) / 4;
-  a.xs = vec == 8 ? 0 : 5;
-  while (a.xs < 8 && (1 << a.xs) < want) ++a.xs;
-  const int rows = (kThreads >> a.xs) * (vec == 8 ? lookup_rows<W, 8>() : lookup_rows<W, 1>());
+  // threads of a row: as many as it has units, or a quarter where a thread takes four of them; equal parts where a CTA has fewer
+  const int units = c.D / vec, want = vec == 8 ? units : (units + 3) / 4, times = (want + kThreads - 1) / kThreads;
+  a.X = (want + times - 1) / times, a.Y = kThreads / a.X, a.xs = 0;
+  while (1 << a.xs < a.X) ++a.xs;
+  const int rows = a.Y * (vec == 8 ? lookup_rows<W, 8>() : lookup_rows<W, 1>());
   const dim3 grid((unsigned)((c.T + rows - 1) / rows), (unsigned)c.K);
-  if (vec == 8) k_embed_lookup<W, O, 8><<<grid, kThreads, 0, s>>>(a);
-  else if (vec == 2) k_embed_lookup<W, O, 2><<<grid, kThreads, 0, s>>>(a);
-  else k_embed_lookup<W, O, 1><<<grid, kThreads, 0, s>>>(a);
+  if (vec == 8 && kThreads >> a.xs == a.Y) k_embed_lookup<W, O, 8, true><<<grid, kThreads, 0, s>>>(a);
+  else if (vec == 8) k_embed_lookup<W, O, 8, false><<<grid, kThreads, 0, s>>>(a);
+  else if (vec == 2) k_embed_lookup<W, O, 2, false><<<grid, kThreads, 0, s>>>(a);
+  else k_embed_lookup<W, O, 1, false><<<grid, kThreads, 0, s>>>(a);
 }
 
 // on the stream, after the kernel before it has ended, but set up while that runs
